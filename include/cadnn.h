@@ -157,6 +157,108 @@ cadnn_status cadnn_sparse_fc(const cadnn_weights* w, const void* x, void* y, int
 /* Uploads the device arrays cadnn_sparse_fc needs (otherwise done on its first call). */
 cadnn_status cadnn_fc_prepare(const cadnn_weights* w);
 
+/* Activations of the layers below: `act` arguments take one of these. */
+#define CADNN_ACT_NONE 0
+#define CADNN_ACT_RELU 1
+#define CADNN_ACT_SILU 2         /* v / (1 + exp(-v)) */
+
+/* ------------------------------------------------------------------------- *
+ * Fully connected layer with 4-bit weights (Section 3: weight quantisation, the other half of
+ * the compression, restricts a layer's weights to a few levels).  A weight is a code -8..7 times
+ * the scale of its group of `group` consecutive inputs of its filter:
+ *
+ *   y[t][o] = act( sum_g scales[o][g] * sum_{i in group g} codes[o][i] * x[t][i] + bias[o] )
+ *
+ * groups = ceil(cin / group), the last one may be short.  A group's sum is taken in fp32 over exact
+ * codes and multiplied by its scale there: no weight is rounded.  fp32 activations keep all of their
+ * bits (those of values below 2^-110 in magnitude may not all count).  Unlike a pruned weight, a code
+ * of zero does meet its activation: 0 * infinity is no number.
+ * cadnn_q4_pack quantises the HOST tensor [cout][cin] to the nearest code; a group's scale is its largest
+ * magnitude / 7.  cadnn_q4_pack_codes takes HOST codes [cout][cin] and scales [cout][groups] that
+ * some quantisation has made.  For CADNN_F16 the scales are rounded to the nearest binary16 (before the
+ * codes are chosen).  Packing is pure host work; the device layout is uploaded by the first call, to the
+ * device that is current then, or by cadnn_q4_prepare; the handle stays on that device.
+ * Errors: EINVAL (NULL pointer, non-positive size, unknown dtype, a code outside -8..7, a weight or scale
+ * that is not finite or of 2^120 and more, or beyond binary16 for CADNN_F16); EUNSUPPORTED (group other than
+ * 32, 64, 128; cin or cout above 2^24); ENOMEM.  *out is set to NULL on failure.
+ * ------------------------------------------------------------------------- */
+typedef struct cadnn_q4_weights cadnn_q4_weights;
+cadnn_status cadnn_q4_pack(const float* w_host, int cout, int cin, int group, cadnn_dtype dtype, cadnn_q4_weights** out);
+cadnn_status cadnn_q4_pack_codes(const int8_t* codes_host, const float* scales_host, int cout, int cin, int group,
+                                 cadnn_dtype dtype, cadnn_q4_weights** out);
+cadnn_status cadnn_q4_free(cadnn_q4_weights* w);      /* NULL is accepted */
+/* The codes [cout][cin] and the scales [cout][groups], as stored, to HOST arrays (either may be NULL). */
+cadnn_status cadnn_q4_export(const cadnn_q4_weights* w, int8_t* codes, float* scales);
+/* The dense HOST tensor [cout][cin] that the codes and scales stand for. */
+cadnn_status cadnn_q4_unpack(const cadnn_q4_weights* w, float* w_host_out);
+cadnn_status cadnn_q4_prepare(const cadnn_q4_weights* w);
+/* x: device, n rows of cin elements, x_stride >= cin elements from one row to the next; y: device, n rows
+ * of cout elements, y_stride apart (what lies between its rows is left alone); both of the handle's type;
+ * bias: device fp32 [cout] or NULL.  y must not overlap x.  Asynchronous on `stream`, allocates nothing but on a first call, which
+ * a captured stream refuses (EINVAL).  Rows that start at multiples of 16 bytes are read fastest.
+ * Errors: EINVAL (NULL pointer, n <= 0, a stride below its row, unknown act, a misaligned pointer, weights on
+ * another device than the current one); EUNSUPPORTED (n above 2^24); EHIP. */
+cadnn_status cadnn_q4_fc(const cadnn_q4_weights* w, const void* x, int64_t x_stride, void* y, int64_t y_stride, int n,
+                         const void* bias, int act, void* stream);
+
+/* ------------------------------------------------------------------------- *
+ * Layers on packed sequences (no passage of the paper to cite: its models are image networks; these
+ * are the depthwise convolution and the recurrence of a sequence model whose other layers are
+ * the products above).  `tokens` rows of `channels` elements hold `seqs` sequences, one behind the other.
+ * seq_start: DEVICE array of seqs + 1 ascending offsets -- sequence s is rows seq_start[s] up to
+ * seq_start[s + 1] -- or NULL: every sequence has tokens / seqs rows.  Sequences may be empty (their state
+ * is left alone), and rows that belong to none are neither read into an output nor written.  The offsets are read on the device, in
+ * stream order; values outside [0, tokens] are cut to it, and an end before its start is an empty sequence.
+ * Rows lie `*_stride` elements apart.  tokens = 0 is a call that does nothing.
+ * A state is kept by the caller, one per sequence, read when the call begins and replaced by what the
+ * sequence ends with: a prompt in one call, in several, or token by token leads to the same values.  NULL: every
+ * sequence starts from zero and nothing is kept.
+ * ------------------------------------------------------------------------- */
+/* Short causal depthwise convolution:
+ *
+ *   y[t][c] = act( sum_{j < taps} w[c][j] * x~[t - (taps - 1) + j][c] + bias[c] )
+ *
+ * x~ before the first row of a sequence is its state, device [seqs][taps - 1][channels] of the handle's
+ * type: the last taps - 1 rows of what came before, the newest last.  w: a handle packed from the HOST
+ * tensor [channels][1][1][taps], as for cadnn_depthwise_conv2d; taps that are exactly zero are skipped.
+ * bias: device fp32 [channels] or NULL.  x, y and state must not overlap.  The first call uploads the filter
+ * table (cadnn_depthwise_prepare), which a captured stream refuses (EINVAL).
+ * Errors: EINVAL (NULL pointer, negative tokens, seqs <= 0, tokens that are no multiple of seqs without seq_start, a stride below the number
+ * of channels, unknown act, a misaligned pointer, a handle that is no such bank); EUNSUPPORTED (more than 8
+ * taps, 2^23 channels, 2^24 sequences or 2^30 tokens); EHIP. */
+cadnn_status cadnn_causal_conv1d(const cadnn_weights* w, const void* x, int64_t x_stride, void* y, int64_t y_stride,
+                                 int tokens, int seqs, const int32_t* seq_start, void* state, const void* bias,
+                                 int act, void* stream);
+
+/* Selective state space scan: for every row t, channel c and state n < dstate
+ *
+ *   step = dt[t][c] + dt_bias[c], and log(1 + exp(step)) of that if `softplus`
+ *   h[c][n] = exp(step * a[c][n]) * h[c][n] + step * x[t][c] * b[t][g][n]      g = c / (channels / groups)
+ *   y[t][c] = (sum_n c[t][g][n] * h[c][n] + d[c] * x[t][c]) * silu(z[t][c])
+ *
+ * x, dt, z, y: rows of `channels` elements; b, c: rows of groups * dstate elements, all of type dtype.
+ * a: fp32 [channels][dstate]; d, dt_bias: fp32 [channels] or NULL (0); z: NULL for no gate.  state: fp32
+ * [seqs][channels][dstate] or NULL.  Sums and states are fp32.  y must not overlap what is read.  All of it in
+ * memory of the current device.
+ * workspace: device memory of cadnn_selective_scan_workspace_bytes bytes (0 for many calls), used by this call alone until it is through: long
+ * sequences that are too few to fill the chip are cut into pieces that run side by side.  Without it, or with
+ * less, every sequence is worked on from end to end: slower, and with differently rounded sums.
+ * Errors: EINVAL (NULL pointer, bad sizes or strides as above, channels that are no multiple of groups, a
+ * misaligned pointer, unknown dtype); EUNSUPPORTED (dstate above 256, more than 2^20 channels, 4096 groups, 65535 sequences or
+ * 2^30 tokens); EHIP. */
+typedef struct cadnn_scan_args {
+    cadnn_dtype dtype;
+    int tokens, seqs, channels, dstate, groups, softplus;
+    const int32_t* seq_start;
+    const void *x, *dt, *b, *c, *z;
+    void* y;
+    int64_t x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride;
+    const float *a, *d, *dt_bias;
+    float* state;
+} cadnn_scan_args;
+cadnn_status cadnn_selective_scan_workspace_bytes(const cadnn_scan_args* args, size_t* bytes);
+cadnn_status cadnn_selective_scan(const cadnn_scan_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------------- *
  * Fused depthwise convolution layer (Section 4 names depthwise convolution +
  * batch-norm + activation, as in MobileNet-V1, among the fused kernels): each

@@ -9,6 +9,9 @@ import numpy as np
 
 F32 = 0
 F16 = 1
+ACT_NONE = 0
+ACT_RELU = 1
+ACT_SILU = 2
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 # CADNN_LIB_PATH: another build of the same library (the host-sanitizer build); never a fallback
@@ -19,6 +22,8 @@ _vp = ctypes.c_void_p
 _i = ctypes.c_int
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _f32p = ctypes.POINTER(ctypes.c_float)
+_i8p = ctypes.POINTER(ctypes.c_int8)
+_i64 = ctypes.c_int64
 
 _STATUS = {0: "CADNN_OK", 1: "CADNN_EINVAL", 2: "CADNN_EUNSUPPORTED", 3: "CADNN_ENOMEM", 4: "CADNN_EHIP"}
 
@@ -43,6 +48,15 @@ class PlanInfo(ctypes.Structure):
     """Mirror of cadnn_plan_info."""
     _fields_ = [("entries", ctypes.c_int64), ("stream_bytes", ctypes.c_int64), ("alloc_bytes", ctypes.c_int64), ("table_bytes", ctypes.c_int64),
                 ("bytes_per_nonzero", ctypes.c_double), ("chunks", ctypes.c_int), ("lds_bytes", ctypes.c_int)]
+
+
+class ScanArgs(ctypes.Structure):
+    """Mirror of cadnn_scan_args."""
+    _fields_ = [("dtype", ctypes.c_int), ("tokens", ctypes.c_int), ("seqs", ctypes.c_int), ("channels", ctypes.c_int),
+                ("dstate", ctypes.c_int), ("groups", ctypes.c_int), ("softplus", ctypes.c_int), ("seq_start", _vp),
+                ("x", _vp), ("dt", _vp), ("b", _vp), ("c", _vp), ("z", _vp), ("y", _vp),
+                ("x_stride", _i64), ("dt_stride", _i64), ("b_stride", _i64), ("c_stride", _i64), ("z_stride", _i64),
+                ("y_stride", _i64), ("a", _vp), ("d", _vp), ("dt_bias", _vp), ("state", _vp)]
 
 
 def lib_path() -> str:
@@ -82,6 +96,16 @@ def lib() -> ctypes.CDLL:
         "cadnn_fc_prepare": (_i, [_vp]),
         "cadnn_depthwise_conv2d": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _vp, _i, _vp]),
         "cadnn_depthwise_prepare": (_i, [_vp]),
+        "cadnn_q4_pack": (_i, [_f32p, _i, _i, _i, _i, ctypes.POINTER(_vp)]),
+        "cadnn_q4_pack_codes": (_i, [_i8p, _f32p, _i, _i, _i, _i, ctypes.POINTER(_vp)]),
+        "cadnn_q4_free": (_i, [_vp]),
+        "cadnn_q4_export": (_i, [_vp, _i8p, _f32p]),
+        "cadnn_q4_unpack": (_i, [_vp, _f32p]),
+        "cadnn_q4_prepare": (_i, [_vp]),
+        "cadnn_q4_fc": (_i, [_vp, _vp, _i64, _vp, _i64, _i, _vp, _i, _vp]),
+        "cadnn_causal_conv1d": (_i, [_vp, _vp, _i64, _vp, _i64, _i, _i, _vp, _vp, _vp, _i, _vp]),
+        "cadnn_selective_scan_workspace_bytes": (_i, [ctypes.POINTER(ScanArgs), ctypes.POINTER(ctypes.c_size_t)]),
+        "cadnn_selective_scan": (_i, [ctypes.POINTER(ScanArgs), _vp, ctypes.c_size_t, _vp]),
         "cadnn_device_copy": (_i, [_vp, _vp, ctypes.c_size_t, _vp]),
         "cadnn_maxpool2d": (_i, [_vp, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _vp]),
         "cadnn_avgpool2d": (_i, [_vp, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _vp]),
@@ -320,6 +344,255 @@ def cadnn_sparse_fc(w: Weights, x, bias=None, relu: bool = False, out=None, stre
 
 def cadnn_fc_prepare(w: Weights) -> None:
     _check(lib().cadnn_fc_prepare(w.handle))
+
+
+class Q4Weights:
+    """Owner of a cadnn_q4_weights handle."""
+
+    def __init__(self, handle: int, cout: int, cin: int, group: int, dtype: int):
+        self.handle = handle
+        self.cout, self.cin, self.group, self.dtype = cout, cin, group, dtype
+
+    @property
+    def groups(self) -> int:
+        return -(-self.cin // self.group)
+
+    def free(self) -> None:
+        if self.handle:
+            lib().cadnn_q4_free(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def cadnn_q4_pack(w: np.ndarray, group: int = 128, dtype: int = F32) -> Q4Weights:
+    """Quantises [cout][cin] weights to codes -8..7, one scale per `group` inputs of a filter."""
+    w = np.ascontiguousarray(w, dtype=np.float32)
+    if w.ndim != 2:
+        raise ValueError("weights are not a matrix")
+    out = _vp()
+    _check(lib().cadnn_q4_pack(w.ctypes.data_as(_f32p), w.shape[0], w.shape[1], group, dtype, ctypes.byref(out)))
+    return Q4Weights(out.value, w.shape[0], w.shape[1], group, dtype)
+
+
+def cadnn_q4_pack_codes(codes: np.ndarray, scales: np.ndarray, group: int = 128, dtype: int = F32) -> Q4Weights:
+    """codes: integers -8..7 [cout][cin]; scales: [cout][ceil(cin / group)]."""
+    codes = np.asarray(codes)
+    if codes.ndim != 2 or codes.dtype.kind not in "iu":
+        raise ValueError("codes are not a matrix of integers")
+    if codes.dtype != np.int8 and codes.size and (codes.min() < -8 or codes.max() > 7):
+        raise ValueError("a code outside -8..7")
+    codes = np.ascontiguousarray(codes, dtype=np.int8)
+    scales = np.ascontiguousarray(scales, dtype=np.float32)
+    if group > 0 and scales.shape != (codes.shape[0], -(-codes.shape[1] // group)):
+        raise ValueError("scales are not [cout][ceil(cin / group)]")
+    out = _vp()
+    _check(lib().cadnn_q4_pack_codes(codes.ctypes.data_as(_i8p), scales.ctypes.data_as(_f32p), codes.shape[0], codes.shape[1],
+                                     group, dtype, ctypes.byref(out)))
+    return Q4Weights(out.value, codes.shape[0], codes.shape[1], group, dtype)
+
+
+def cadnn_q4_free(w: Q4Weights) -> None:
+    w.free()
+
+
+def cadnn_q4_export(w: Q4Weights):
+    codes = np.empty((w.cout, w.cin), np.int8)
+    scales = np.empty((w.cout, w.groups), np.float32)
+    _check(lib().cadnn_q4_export(w.handle, codes.ctypes.data_as(_i8p), scales.ctypes.data_as(_f32p)))
+    return {"codes": codes, "scales": scales}
+
+
+def cadnn_q4_unpack(w: Q4Weights) -> np.ndarray:
+    out = np.empty((w.cout, w.cin), np.float32)
+    _check(lib().cadnn_q4_unpack(w.handle, out.ctypes.data_as(_f32p)))
+    return out
+
+
+def cadnn_q4_prepare(w: Q4Weights) -> None:
+    _check(lib().cadnn_q4_prepare(w.handle))
+
+
+def _rows(t, name: str, dtype, shape, device=None):
+    """A tensor whose rows are contiguous (a slice of a wider one may be): its distance between rows."""
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} is not a CUDA tensor {list(shape)} of {dtype}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on another device than the other tensors")
+    if t.is_contiguous():
+        return t.numel() // t.shape[0] if t.shape[0] else 1
+    inner = 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size != 1 and stride != inner:
+            raise ValueError(f"the rows of {name} are not contiguous")
+        inner *= size
+    return max(int(t.stride(0)), inner) if t.shape[0] == 1 else int(t.stride(0))
+
+
+def _whole(t, name: str, dtype, shape, device) -> None:
+    if not t.is_cuda or t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} is not a contiguous tensor {list(shape)} of {dtype} on {device}")
+
+
+class _On:
+    """Makes the tensors' device and the call's stream (`stream`, or that device's current one) the
+    current ones: what is allocated inside belongs to that stream.  `mark` keeps the memory of
+    tensors of another stream from being handed out again before the call is through."""
+    __slots__ = ("_device", "_stream", "_context", "_foreign", "ptr")
+
+    def __init__(self, device, stream):
+        self._device, self._stream, self._context, self._foreign = device, stream, None, False
+
+    def __enter__(self):
+        import torch
+        if self._stream is None and self._device.index == torch.cuda.current_device():
+            self.ptr = int(torch.cuda.current_stream().cuda_stream)
+            return self
+        if self._stream is not None and self._stream.device != self._device:
+            raise ValueError("the stream belongs to another device than the tensors")
+        current = torch.cuda.current_stream(self._device)
+        s = current if self._stream is None else self._stream
+        self._foreign = s != current
+        self._context = torch.cuda.stream(s)
+        self._context.__enter__()
+        self.ptr = int(s.cuda_stream)
+        return self
+
+    def mark(self, *tensors) -> None:
+        if self._foreign:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self._stream)
+
+    def __exit__(self, *exc):
+        if self._context is not None:
+            self._context.__exit__(*exc)
+
+
+def cadnn_q4_fc(w: Q4Weights, x, bias=None, act: int = ACT_NONE, out=None, stream=None):
+    """x: CUDA tensor [n][cin] with contiguous rows (a slice of a wider tensor may be passed); returns (or fills) [n][cout]."""
+    import torch
+    dtype = _torch_dtype(w.dtype)
+    if x.dim() != 2 or x.shape[1] != w.cin:
+        raise ValueError("feature mismatch")
+    n = x.shape[0]
+    x_stride = _rows(x, "x", dtype, (n, w.cin))
+    if bias is not None:
+        _whole(bias, "bias", torch.float32, (w.cout,), x.device)
+    y_stride = w.cout if out is None else _rows(out, "out", dtype, (n, w.cout), x.device)
+    with _On(x.device, stream) as on:
+        on.mark(x, bias, out)
+        if out is None:
+            out = torch.empty((n, w.cout), dtype=dtype, device=x.device)
+        _check(lib().cadnn_q4_fc(w.handle, _dptr(x), x_stride, _dptr(out), y_stride, n, _dptr(bias), act, on.ptr))
+    return out
+
+
+def cadnn_causal_conv1d(w: Weights, x, state=None, seq_start=None, seqs: int = 1, bias=None, act: int = ACT_NONE,
+                        out=None, stream=None):
+    """w packed from [channels][1][1][taps]; x: CUDA tensor [tokens][channels] with contiguous rows; state: [seqs][taps - 1][channels],
+    replaced; seq_start: int32 [seqs + 1] on the device (None: sequences of one length)."""
+    import torch
+    dtype = _torch_dtype(w.dtype)
+    if x.dim() != 2 or x.shape[1] != w.cout:
+        raise ValueError("channel mismatch")
+    tokens = x.shape[0]
+    x_stride = _rows(x, "x", dtype, (tokens, w.cout))
+    if state is not None:
+        _whole(state, "state", dtype, (seqs, w.kw - 1, w.cout), x.device)
+    if seq_start is not None:
+        _whole(seq_start, "seq_start", torch.int32, (seqs + 1,), x.device)
+    if bias is not None:
+        _whole(bias, "bias", torch.float32, (w.cout,), x.device)
+    y_stride = w.cout if out is None else _rows(out, "out", dtype, (tokens, w.cout), x.device)
+    with _On(x.device, stream) as on:
+        on.mark(x, state, seq_start, bias, out)
+        if out is None:
+            out = torch.empty((tokens, w.cout), dtype=dtype, device=x.device)
+        _check(lib().cadnn_causal_conv1d(w.handle, _dptr(x), x_stride, _dptr(out), y_stride, tokens, seqs, _dptr(seq_start),
+                                         _dptr(state), _dptr(bias), act, on.ptr))
+    return out
+
+
+def _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, out) -> ScanArgs:
+    import torch
+    if x.dim() != 2 or x.dtype not in (torch.float32, torch.float16):
+        raise ValueError("x is not a float32 or float16 tensor [tokens][channels]")
+    tokens, channels = x.shape
+    if a.dim() != 2 or a.shape[0] != channels:
+        raise ValueError("a is not [channels][dstate]")
+    dstate = a.shape[1]
+    if b.dim() == 2:
+        b = b.unsqueeze(1)
+    if c.dim() == 2:
+        c = c.unsqueeze(1)
+    if b.dim() != 3:
+        raise ValueError("b is not [tokens][groups][dstate]")
+    groups = b.shape[1]
+    g = ScanArgs()
+    g.dtype = F16 if x.dtype == torch.float16 else F32
+    g.tokens, g.seqs, g.channels, g.dstate, g.groups, g.softplus = tokens, seqs, channels, dstate, groups, int(bool(softplus))
+    wide, narrow = (tokens, channels), (tokens, groups, dstate)
+    g.x_stride = _rows(x, "x", x.dtype, wide)
+    g.dt_stride = _rows(dt, "dt", x.dtype, wide, x.device)
+    g.b_stride = _rows(b, "b", x.dtype, narrow, x.device)
+    g.c_stride = _rows(c, "c", x.dtype, narrow, x.device)
+    _whole(a, "a", torch.float32, (channels, dstate), x.device)
+    for name, v in (("d", d), ("dt_bias", dt_bias)):
+        if v is not None:
+            _whole(v, name, torch.float32, (channels,), x.device)
+    if z is not None:
+        g.z_stride = _rows(z, "z", x.dtype, wide, x.device)
+    if state is not None:
+        _whole(state, "state", torch.float32, (seqs, channels, dstate), x.device)
+    if seq_start is not None:
+        _whole(seq_start, "seq_start", torch.int32, (seqs + 1,), x.device)
+    if out is not None:
+        g.y_stride = _rows(out, "out", x.dtype, wide, x.device)
+        g.y = _dptr(out)
+    g.x, g.dt, g.a, g.b, g.c, g.d, g.z = (_dptr(v) for v in (x, dt, a, b, c, d, z))
+    g.dt_bias, g.state, g.seq_start = _dptr(dt_bias), _dptr(state), _dptr(seq_start)
+    return g
+
+
+def cadnn_selective_scan_workspace_bytes(x, dt, a, b, c, d=None, z=None, dt_bias=None, softplus: bool = False, state=None,
+                                         seq_start=None, seqs: int = 1) -> int:
+    """Bytes of workspace with which cadnn_selective_scan works on long sequences in pieces."""
+    g = _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, None)
+    nbytes = ctypes.c_size_t()
+    _check(lib().cadnn_selective_scan_workspace_bytes(ctypes.byref(g), ctypes.byref(nbytes)))
+    return int(nbytes.value)
+
+
+def cadnn_selective_scan(x, dt, a, b, c, d=None, z=None, dt_bias=None, softplus: bool = False, state=None, seq_start=None,
+                         seqs: int = 1, out=None, workspace=None, stream=None):
+    """x, dt, z: CUDA tensors [tokens][channels]; b, c: [tokens][groups][dstate] or [tokens][dstate]; a: [channels][dstate]; state:
+    [seqs][channels][dstate], replaced.  workspace: a uint8 tensor (None: one is taken from torch's allocator for the call; an empty one:
+    no workspace)."""
+    import torch
+    g = _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, out)
+    if workspace is not None and (not workspace.is_cuda or workspace.device != x.device or workspace.dtype != torch.uint8 or not workspace.is_contiguous()):
+        raise ValueError(f"workspace is not a contiguous uint8 tensor on {x.device}")
+    with _On(x.device, stream) as on:
+        on.mark(x, dt, a, b, c, d, z, dt_bias, state, seq_start, out, workspace)
+        if out is None:
+            out = torch.empty(tuple(x.shape), dtype=x.dtype, device=x.device)
+            g.y, g.y_stride = _dptr(out), x.shape[1]
+        size = 0
+        if workspace is None:
+            nbytes = ctypes.c_size_t()
+            _check(lib().cadnn_selective_scan_workspace_bytes(ctypes.byref(g), ctypes.byref(nbytes)))
+            size = nbytes.value
+            if size:
+                workspace = torch.empty(size, dtype=torch.uint8, device=x.device)
+        else:
+            size = workspace.numel()
+        _check(lib().cadnn_selective_scan(ctypes.byref(g), _dptr(workspace) if size else None, size, on.ptr))
+    return out
 
 
 def cadnn_device_copy(src, dst, stream=None) -> None:

@@ -1,0 +1,254 @@
+// Fully connected layer with 4-bit weights and one scale per group of inputs:
+//
+//   y[t][o] = act( sum_g s[o][g] * sum_{i in g} q[o][i] * x[t][i] + bias[o] ),   q in -8 .. 7
+//
+// The codes reach the matrix instructions as what they are, small integers, exact in fp16 and bf16; a group's sum is
+// taken in fp32 and multiplied by its scale there, so that no weight is ever rounded.  fp32 activations are cut into three
+// bf16 parts that add up to them exactly (8 bits each of 24), one matrix instruction per part.
+#include "q4.h"
+
+namespace cadnn {
+
+namespace {
+
+typedef _Float16 q4_h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 q4_h4 __attribute__((ext_vector_type(4)));
+typedef _Float16 q4_h2 __attribute__((ext_vector_type(2)));
+typedef __bf16 q4_b8 __attribute__((ext_vector_type(8)));
+typedef float q4_f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t q4_u4 __attribute__((ext_vector_type(4)));
+
+struct Q4Args {
+    const uint32_t* codes;
+    const void* scales;
+    const void* x;
+    void* y;
+    const float* bias;
+    int64_t x_stride, y_stride;
+    int n, cin, cout, blocks, act;
+    int y_vec;      // rows of y are aligned for stores of four elements
+};
+
+// Eight codes of one lane as the left operand of a matrix instruction.
+template <typename T> struct Q4Frag;
+template <> struct Q4Frag<_Float16> {
+    static constexpr int kParts = 1;
+    typedef q4_h8 V;
+    // 0x6400 | u is 1024 + u in fp16 and 0x6400 | 16 u is 1024 + 16 u: a subtraction, or a multiplication by 1/16 and a
+    // subtraction, both exact, leave u - 8.
+    static __device__ __forceinline__ V codes(uint32_t w) {
+        const q4_h2 m = {(_Float16)1032.0f, (_Float16)1032.0f}, s = {(_Float16)0.0625f, (_Float16)0.0625f}, k = {(_Float16)72.0f, (_Float16)72.0f};
+        const uint32_t v = w >> 8;
+        union { V v8; q4_h2 v2[4]; } r;
+        r.v2[0] = __builtin_bit_cast(q4_h2, (w & 0x000f000fu) | 0x64006400u) - m;
+        r.v2[1] = __builtin_elementwise_fma(__builtin_bit_cast(q4_h2, (w & 0x00f000f0u) | 0x64006400u), s, -k);
+        r.v2[2] = __builtin_bit_cast(q4_h2, (v & 0x000f000fu) | 0x64006400u) - m;
+        r.v2[3] = __builtin_elementwise_fma(__builtin_bit_cast(q4_h2, (v & 0x00f000f0u) | 0x64006400u), s, -k);
+        return r.v8;
+    }
+    static __device__ __forceinline__ void parts(const _Float16 (&v)[8], V (&out)[1]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[0][e] = v[e];
+    }
+    static __device__ __forceinline__ q4_f4 mul(V a, V b, q4_f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Q4Frag<float> {
+    static constexpr int kParts = 3;
+    typedef q4_b8 V;
+    // (codes as sixteenths: what the conversion of a signed nibble gives; the scales on the device are 16 times theirs)
+    static __device__ __forceinline__ V codes(uint32_t w) {
+        w ^= 0x88888888u;
+        union { V v8; uint32_t u[4]; } r;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const uint32_t lo = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(w >> (4 * t))));
+            const uint32_t hi = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(w >> (16 + 4 * t))));
+            r.u[t] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+        }
+        return r.v8;
+    }
+    // The parts are cut off, not rounded, so that a large value's first part stays finite; what is left of an infinity
+    // (no number) is replaced by a finite value that the infinity swallows.
+    static __device__ __forceinline__ void parts(const float (&v)[8], V (&out)[3]) {
+        union { V v8; uint32_t u[4]; } p[3];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            float lo = v[2 * t], hi = v[2 * t + 1];
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                p[k].u[t] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+                lo -= __uint_as_float(p[k].u[t] << 16);
+                hi -= __uint_as_float(p[k].u[t] & 0xffff0000u);
+                if (k == 0) {
+                    lo = __builtin_amdgcn_fmed3f(lo, -0x1p121f, 0x1p121f);
+                    hi = __builtin_amdgcn_fmed3f(hi, -0x1p121f, 0x1p121f);
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) out[k] = p[k].v8;
+    }
+    static __device__ __forceinline__ q4_f4 mul(V a, V b, q4_f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+
+// Four scales of a lane's filters.
+__device__ __forceinline__ q4_f4 q4_scales(const _Float16* p) {
+    const q4_h4 v = *(const q4_h4*)p;
+    return (q4_f4){(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
+}
+__device__ __forceinline__ q4_f4 q4_scales(const float* p) { return *(const q4_f4*)p; }
+
+// Eight activations from input i0 on; what lies behind the row's end, or in no row, is zero.
+template <typename T, bool VEC>
+__device__ __forceinline__ void q4_load_x(const T* row, int i0, int cin, bool real, T (&v)[8]) {
+    if (VEC && i0 + 8 <= cin) {
+        typedef T V __attribute__((ext_vector_type(16 / sizeof(T))));
+        constexpr int N = 16 / (int)sizeof(T);
+#pragma unroll
+        for (int k = 0; k < 8; k += N) {
+            V p = {};
+            if (real) p = *(const V*)(row + i0 + k);
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[k + e] = p[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = real && i0 + e < cin ? row[i0 + e] : (T)0.0f;
+    }
+}
+
+// The end of a tile: four filters of one token.
+template <typename T>
+__device__ __forceinline__ void q4_store(const Q4Args& a, int token, int o0, q4_f4 v) {
+    if (token >= a.n || o0 >= a.cout) return;
+    T* out = (T*)a.y + (int64_t)token * a.y_stride + o0;
+    if (a.y_vec && o0 + 4 <= a.cout) {
+        typedef T V __attribute__((ext_vector_type(4)));
+        V r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = (T)apply_act(v[e] + (a.bias ? a.bias[o0 + e] : 0.0f), a.act);
+        *(V*)out = r;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (o0 + e < a.cout) out[e] = (T)apply_act(v[e] + (a.bias ? a.bias[o0 + e] : 0.0f), a.act);
+    }
+}
+
+// Few tokens: the weights are read once and bound the kernel.  A workgroup owns 16 * RT filters and 16 * NT tokens and its
+// waves split the inputs, block by block in turn, so that even one tile of filters is read by eight waves; their sums meet
+// in LDS and are added in the waves' order.
+template <typename T, int GP, int RT, int NT, bool VEC>
+__global__ __launch_bounds__(512) void q4_few_kernel(const Q4Args a) {
+    typedef Q4Frag<T> F;
+    extern __shared__ __attribute__((aligned(16))) char q4_smem[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int j = lane & 15, g = lane >> 4;
+    const int tile0 = blockIdx.x * RT, tiles = (a.cout + 15) / 16;
+    const int token0 = blockIdx.y * 16 * NT;
+    q4_f4 acc[RT][NT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[r][t] = (q4_f4){0.0f, 0.0f, 0.0f, 0.0f};
+    const T* rows[NT];
+    bool real[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int token = token0 + 16 * t + j;
+        real[t] = token < a.n;
+        rows[t] = (const T*)a.x + (int64_t)(real[t] ? token : 0) * a.x_stride;
+    }
+    for (int b = wave; b < a.blocks; b += waves) {
+        q4_u4 w[RT];
+        q4_f4 sc[RT][GP];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const int tile = min(tile0 + r, tiles - 1);
+            w[r] = *(const q4_u4*)(a.codes + ((int64_t)tile * a.blocks + b) * 256 + lane * 4);
+#pragma unroll
+            for (int p = 0; p < GP; ++p) sc[r][p] = q4_scales((const T*)a.scales + (((int64_t)tile * a.blocks + b) * GP + p) * 16 + 4 * g);
+        }
+        typename F::V xf[NT][4][F::kParts];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                T v[8];
+                q4_load_x<T, VEC>(rows[t], b * 128 + s * 32 + g * 8, a.cin, real[t], v);
+                F::parts(v, xf[t][s]);
+            }
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            q4_f4 sum[NT];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const typename F::V c = F::codes(w[r][s]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    if (s % (4 / GP) == 0) sum[t] = (q4_f4){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int p = F::kParts - 1; p >= 0; --p) sum[t] = F::mul(c, xf[t][s][p], sum[t]);
+                    if ((s + 1) % (4 / GP) == 0) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[r][t][e] = fmaf(sc[r][s / (4 / GP)][e], sum[t][e], acc[r][t][e]);
+                    }
+                }
+            }
+        }
+    }
+    q4_f4* part = (q4_f4*)q4_smem;       // [wave][r][t][lane]
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) part[((wave * RT + r) * NT + t) * 64 + lane] = acc[r][t];
+    __syncthreads();
+    for (int i = wave; i < RT * NT; i += waves) {
+        q4_f4 v = part[i * 64 + lane];
+        for (int k = 1; k < waves; ++k) v += part[(k * RT * NT + i) * 64 + lane];
+        q4_store<T>(a, token0 + 16 * (i % NT) + j, (tile0 + i / NT) * 16 + 4 * g, v);
+    }
+}
+
+template <typename T, int GP, int RT, int NT>
+hipError_t launch_few(const Q4Args& a, bool vec, hipStream_t s) {
+    const int tiles = (a.cout + 15) / 16;
+    const int waves = a.blocks >= 8 ? 8 : a.blocks;
+    const dim3 grid((unsigned)((tiles + RT - 1) / RT), (unsigned)((a.n + 16 * NT - 1) / (16 * NT)));
+    const size_t lds = (size_t)waves * RT * NT * 64 * sizeof(q4_f4);
+    if (vec) CADNN_LAUNCH((q4_few_kernel<T, GP, RT, NT, true>), grid, dim3(64u * waves), lds, s, a);
+    else CADNN_LAUNCH((q4_few_kernel<T, GP, RT, NT, false>), grid, dim3(64u * waves), lds, s, a);
+    return hipGetLastError();
+}
+
+template <typename T, int GP>
+hipError_t launch_q4(const Q4Args& a, bool vec, hipStream_t s) {
+    return launch_few<T, GP, 1, 1>(a, vec, s);
+}
+
+template <typename T>
+hipError_t launch_q4_group(const Q4Args& a, int group, bool vec, hipStream_t s) {
+    return group == 128 ? launch_q4<T, 1>(a, vec, s) : group == 64 ? launch_q4<T, 2>(a, vec, s) : launch_q4<T, 4>(a, vec, s);
+}
+
+}  // namespace
+
+cadnn_status launch_q4_fc(const cadnn_q4_weights* w, const void* x, int64_t x_stride, void* y, int64_t y_stride, int n,
+                          const float* bias, int act, hipStream_t s) {
+    const size_t e = w->elem();
+    // a launch has at most 65535 rows of workgroups
+    const int step = 16 * 65535;
+    for (int n0 = 0; n0 < n; n0 += step) {
+        Q4Args a{};
+        a.codes = (const uint32_t*)w->d_codes.p; a.scales = w->d_scales.p; a.bias = bias;
+        a.x = (const char*)x + (size_t)n0 * x_stride * e; a.y = (char*)y + (size_t)n0 * y_stride * e;
+        a.x_stride = x_stride; a.y_stride = y_stride;
+        a.n = std::min(step, n - n0); a.cin = w->cin; a.cout = w->cout; a.blocks = (w->cin + kQ4Block - 1) / kQ4Block; a.act = act;
+        a.y_vec = (uintptr_t)y % (4 * e) == 0 && y_stride % 4 == 0;
+        const bool vec = (uintptr_t)x % 16 == 0 && (x_stride * (int64_t)e) % 16 == 0;
+        CADNN_HIP(w->dtype == CADNN_F16 ? launch_q4_group<_Float16>(a, w->group, vec, s) : launch_q4_group<float>(a, w->group, vec, s));
+    }
+    return CADNN_OK;
+}
+
+}  // namespace cadnn

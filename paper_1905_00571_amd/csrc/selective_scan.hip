@@ -1,0 +1,447 @@
+// Selective state space scan over packed sequences.  For every token t, channel c and state n
+//
+//   dt = dt_raw[t][c] + dt_bias[c], through softplus if asked
+//   h[c][n] = exp(dt * a[c][n]) * h[c][n] + dt * x[t][c] * b[t][g(c)][n]
+//   y[t][c] = (sum_n c[t][g(c)][n] * h[c][n] + d[c] * x[t][c]) * silu(z[t][c])
+//
+// Every (t, c, n) costs an exponential (a quarter of the vector rate) and four full-rate operations, about 32 cycles of a
+// SIMD per 64 of them, against 2 / N elements of traffic: from N = 16 on the vector units bound a long scan, and the
+// states' traffic a single token.
+#include "sequence.h"
+
+namespace cadnn {
+
+namespace {
+
+constexpr int kScanMaxStates = 256;
+constexpr int kScanTile = 8;          // tokens whose inputs are fetched together
+
+struct SsArgs {
+    const void *x, *dt, *b, *c, *z;
+    void* y;
+    int64_t x_stride, dt_stride, b_stride, c_stride, z_stride, y_stride;
+    const float *a, *d, *dt_bias;
+    float* state;         // [seqs][channels][dstate] or NULL
+    float* part;          // pieces: [slot][channels][dstate], the piece's own end state, later the state it starts from
+    float* span;          // pieces: [slot][channels], the sum of the time steps
+    Sequences q;
+    int channels, dstate, groups, per, softplus;
+    int chunk, blocks_per_group;
+    int64_t slots;
+};
+
+__device__ __forceinline__ float ss_exp2(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// log(1 + exp(v)).  exp(v) from the product v * log2(e) in two parts; below 1/16 the series of log1p, whose first term
+// left out is under 2^-26 of the value, and above it log(u) corrected for the rounding of u = 1 + e.
+__device__ __forceinline__ float ss_softplus(float v) {
+    v = v < -150.0f ? -150.0f : v;      // (exp is zero from there on; the two parts of -infinity would be no numbers)
+    const float hi = v * 1.44269502f, lo = fmaf(v, 1.44269502f, -hi) + v * 1.92596303e-8f;
+    const float e = ss_exp2(hi) * fmaf(lo, 0.693147182f, 1.0f);
+    const float series = e * fmaf(e, fmaf(e, fmaf(e, fmaf(e, fmaf(e, -0.166666672f, 0.2f), -0.25f), 0.333333343f), -0.5f), 1.0f);
+    const float u = 1.0f + e;
+    const float logs = fmaf(__builtin_amdgcn_logf(u), 0.693147182f, (e - (u - 1.0f)) * __builtin_amdgcn_rcpf(u));
+    return v > 20.0f ? v : e < 0.0625f ? series : logs;
+}
+
+__device__ __forceinline__ float ss_silu(float v) {
+    return v * __builtin_amdgcn_rcpf(1.0f + ss_exp2(v * -1.44269502f));
+}
+
+// Sum over the L consecutive lanes that share a channel.
+template <int L>
+__device__ __forceinline__ float ss_sum(float v) {
+    if constexpr (L >= 2) v += __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0xB1, 0xf, 0xf, true));     // lane ^ 1
+    if constexpr (L >= 4) v += __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x4E, 0xf, 0xf, true));     // lane ^ 2
+    if constexpr (L >= 8) v += __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x141, 0xf, 0xf, true));    // mirrored in 8 lanes
+    if constexpr (L >= 16) v += __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x140, 0xf, 0xf, true));   // mirrored in 16 lanes
+    if constexpr (L >= 32) v += __shfl_xor(v, 16, 64);
+    if constexpr (L >= 64) v += __shfl_xor(v, 32, 64);
+    return v;
+}
+
+enum ScanPass {
+    SCAN_WHOLE,     // one pass over whole sequences
+    SCAN_ENDS,      // of every piece: the state it ends with when it starts from zero
+    SCAN_PIECES     // of every piece: its outputs, from the state it starts from
+};
+
+// L lanes hold a channel's states, NS each.  The inputs of kScanTile tokens are fetched while the tile before them is
+// worked on; b and c, which all channels of a group share, go through LDS as fp32.  FULL: dstate = NS * L; else the
+// states behind the last one stay zero whatever x and dt are.
+template <typename T, int NS, int L, int PASS, bool FULL>
+__global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
+    constexpr int CH = 256 / L, N = NS * L, TT = kScanTile;
+    constexpr int ROW = PASS == SCAN_ENDS ? N : 2 * N;          // floats of a token in LDS
+    constexpr int PER = (TT * ROW + 255) / 256;                 // of them fetched by a thread
+    __shared__ __attribute__((aligned(16))) float bc[2][TT * ROW];
+    const int tid = (int)threadIdx.x, sub = tid % L;
+    const int grp = (int)blockIdx.y / a.blocks_per_group;
+    const int in_group = ((int)blockIdx.y - grp * a.blocks_per_group) * CH + tid / L;
+    const bool real = in_group < a.per;
+    const int ch = grp * a.per + (real ? in_group : a.per - 1);
+    int s, lo, hi, t0, t1;
+    const int64_t slot = blockIdx.x;
+    if (PASS == SCAN_WHOLE) {
+        s = (int)slot;
+        seq_range(a.q, s, &lo, &hi);
+        t0 = lo;
+        t1 = hi;
+    } else {
+        int piece;
+        s = seq_of_slot(a.q, (int)slot, a.chunk, &piece);
+        seq_range(a.q, s, &lo, &hi);
+        const int64_t first = lo + (int64_t)piece * a.chunk;
+        if (piece < 0 || first >= hi) return;
+        t0 = (int)first;
+        t1 = (int)min((int64_t)hi, first + a.chunk);
+    }
+    if (t0 >= t1) return;
+    float h[NS], al[NS];
+    float* kept = nullptr;
+    if (PASS == SCAN_WHOLE) kept = a.state ? a.state + ((int64_t)s * a.channels + ch) * a.dstate : nullptr;
+    else kept = a.part + (slot * a.channels + ch) * a.dstate;
+#pragma unroll
+    for (int k = 0; k < NS; ++k) {
+        const int n = sub * NS + k;
+        al[k] = n < a.dstate ? a.a[(int64_t)ch * a.dstate + n] * 1.44269502f : 0.0f;
+        h[k] = PASS != SCAN_ENDS && kept && n < a.dstate ? kept[n] : 0.0f;
+    }
+    const float bias = a.dt_bias ? a.dt_bias[ch] : 0.0f;
+    const float dv = a.d ? a.d[ch] : 0.0f;
+    const T* xp = (const T*)a.x + ch;
+    const T* dp = (const T*)a.dt + ch;
+    const T* zp = (const T*)a.z + ch;
+    T* yp = (T*)a.y + ch;
+    const T* bp = (const T*)a.b + (int64_t)grp * a.dstate;
+    const T* cp = (const T*)a.c + (int64_t)grp * a.dstate;
+    T nx[TT], nd[TT], nz[TT];
+    float nb[PER];
+    auto fetch = [&](int t) {
+#pragma unroll
+        for (int u = 0; u < TT; ++u) {
+            const int at = min(t + u, t1 - 1);
+            nx[u] = xp[(int64_t)at * a.x_stride];
+            nd[u] = dp[(int64_t)at * a.dt_stride];
+            if (PASS != SCAN_ENDS) nz[u] = a.z ? zp[(int64_t)at * a.z_stride] : (T)0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int i = k * 256 + tid, u = i / ROW, r = i % ROW, n = r < N ? r : r - N, at = t + u;
+            float v = 0.0f;
+            if (i < TT * ROW && at < t1 && n < a.dstate)
+                v = r < N ? (float)bp[(int64_t)at * a.b_stride + n] : (float)cp[(int64_t)at * a.c_stride + n];
+            nb[k] = v;
+        }
+    };
+    fetch(t0);
+    float span = 0.0f;
+    int buf = 0;
+    for (int t = t0; t < t1; t += TT, buf ^= 1) {
+        float x[TT], dt[TT], z[TT];
+#pragma unroll
+        for (int u = 0; u < TT; ++u) {
+            x[u] = (float)nx[u];
+            dt[u] = (float)nd[u];
+            z[u] = PASS != SCAN_ENDS ? (float)nz[u] : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if (k * 256 + tid < TT * ROW) bc[buf][k * 256 + tid] = nb[k];
+        __syncthreads();     // (the other buffer is written next, after the next barrier's readers of this one)
+        if (t + TT < t1) fetch(t + TT);
+        const int left = min(TT, t1 - t);
+        float steps = 0.0f;          // (summed by tiles: 8 + chunk / 8 roundings at most, not chunk)
+#pragma unroll
+        for (int u = 0; u < TT; ++u) {
+            if (u < left) {
+                float step = dt[u] + bias;
+                if (a.softplus) step = ss_softplus(step);
+                const float in = step * x[u];
+                const float* row = bc[buf] + u * ROW + sub * NS;
+                float y = 0.0f;
+#pragma unroll
+                for (int k = 0; k < NS; ++k) {
+                    h[k] = fmaf(ss_exp2(step * al[k]), h[k], in * row[k]);
+                    if (!FULL) h[k] = sub * NS + k < a.dstate ? h[k] : 0.0f;
+                    if (PASS != SCAN_ENDS) y = fmaf(row[N + k], h[k], y);
+                }
+                if (PASS == SCAN_ENDS) {
+                    steps += step;
+                } else {
+                    y = ss_sum<L>(y);
+                    y = fmaf(dv, x[u], y);
+                    if (a.z) y *= ss_silu(z[u]);
+                    if (sub == 0 && real) yp[(int64_t)(t + u) * a.y_stride] = (T)y;
+                }
+            }
+        }
+        span += steps;
+    }
+    if (real && kept && PASS != SCAN_PIECES) {
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+            if (sub * NS + k < a.dstate) kept[sub * NS + k] = h[k];
+        if (PASS == SCAN_ENDS && sub == 0) a.span[slot * a.channels + ch] = span;
+    }
+}
+
+// Joins the pieces of each sequence: h = exp(a * span) * h + end, one thread per (sequence, channel, state).  What a piece
+// ended with is replaced by what it starts from; four pieces are fetched at a time.
+__global__ __launch_bounds__(256) void scan_join_kernel(const SsArgs a) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per_seq = (int64_t)a.channels * a.dstate;
+    if (i >= per_seq) return;
+    const int s = (int)blockIdx.y;
+    int lo, hi;
+    seq_range(a.q, s, &lo, &hi);
+    if (lo >= hi) return;
+    const int ch = (int)(i / a.dstate);
+    const int64_t first = seq_first_slot(a.q, s, a.chunk);
+    const int pieces = (int)(((int64_t)hi - lo + a.chunk - 1) / a.chunk);
+    const float al = a.a[i] * 1.44269502f;
+    float* kept = a.state ? a.state + (int64_t)s * per_seq + i : nullptr;
+    float h = kept ? *kept : 0.0f;
+    constexpr int U = 4;
+    for (int p = 0; p < pieces; p += U) {
+        float end[U], span[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t slot = first + min(p + u, pieces - 1);
+            const bool there = slot < a.slots;
+            end[u] = there ? a.part[slot * per_seq + i] : 0.0f;
+            span[u] = there ? a.span[slot * a.channels + ch] : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t slot = first + p + u;
+            if (p + u < pieces && slot < a.slots) {
+                a.part[slot * per_seq + i] = h;
+                // (not below the smallest normal number: an infinite state outlives any number of steps that each shrink it a little)
+                h = fmaf(fmaxf(ss_exp2(al * span[u]), 0x1p-126f), h, end[u]);
+            }
+        }
+    }
+    if (kept) *kept = h;
+}
+
+// Few tokens a sequence: L lanes hold a channel's states, four each, read and written as 16 bytes where they are aligned;
+// b and c come straight from memory.
+template <typename T, int L, bool VEC>
+__global__ __launch_bounds__(256) void scan_few_kernel(const SsArgs a) {
+    const int64_t i = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+    const int sub = (int)threadIdx.x % L, n0 = sub * 4;
+    const bool real = i < (int64_t)a.channels;
+    const int ch = real ? (int)i : a.channels - 1;
+    const int s = (int)blockIdx.y;
+    int lo, hi;
+    seq_range(a.q, s, &lo, &hi);
+    if (lo >= hi) return;
+    const int grp = ch / a.per;
+    float h[4], al[4];
+    float* kept = a.state ? a.state + ((int64_t)s * a.channels + ch) * a.dstate + n0 : nullptr;
+    const float* ap = a.a + (int64_t)ch * a.dstate + n0;
+    typedef float F4 __attribute__((ext_vector_type(4)));
+    const bool whole = VEC && n0 < a.dstate;
+    if (whole) {
+        const F4 av = *(const F4*)ap;
+        F4 hv = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (kept) hv = *(const F4*)kept;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { al[k] = av[k]; h[k] = hv[k]; }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const bool in = n0 + k < a.dstate;
+            al[k] = in ? ap[k] : 0.0f;
+            h[k] = in && kept ? kept[k] : 0.0f;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) al[k] *= 1.44269502f;
+    const float bias = a.dt_bias ? a.dt_bias[ch] : 0.0f;
+    const float dv = a.d ? a.d[ch] : 0.0f;
+    for (int t = lo; t < hi; ++t) {
+        const float x = (float)((const T*)a.x)[(int64_t)t * a.x_stride + ch];
+        float step = (float)((const T*)a.dt)[(int64_t)t * a.dt_stride + ch] + bias;
+        const float z = a.z ? (float)((const T*)a.z)[(int64_t)t * a.z_stride + ch] : 0.0f;
+        const T* bp = (const T*)a.b + (int64_t)t * a.b_stride + (int64_t)grp * a.dstate + n0;
+        const T* cp = (const T*)a.c + (int64_t)t * a.c_stride + (int64_t)grp * a.dstate + n0;
+        float bv[4], cv[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const bool in = n0 + k < a.dstate;
+            bv[k] = in ? (float)bp[k] : 0.0f;
+            cv[k] = in ? (float)cp[k] : 0.0f;
+        }
+        if (a.softplus) step = ss_softplus(step);
+        const float in = step * x;
+        float y = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            h[k] = n0 + k < a.dstate ? fmaf(ss_exp2(step * al[k]), h[k], in * bv[k]) : 0.0f;
+            y = fmaf(cv[k], h[k], y);
+        }
+        y = ss_sum<L>(y);
+        y = fmaf(dv, x, y);
+        if (a.z) y *= ss_silu(z);
+        if (sub == 0 && real) ((T*)a.y)[(int64_t)t * a.y_stride + ch] = (T)y;
+    }
+    if (real && kept) {
+        if (whole) {
+            F4 hv;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) hv[k] = h[k];
+            *(F4*)kept = hv;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (n0 + k < a.dstate) kept[k] = h[k];
+        }
+    }
+}
+
+template <typename T, int NS, int L, int PASS, bool FULL>
+hipError_t launch_scan_pass(const SsArgs& a, hipStream_t s) {
+    const dim3 grid((unsigned)(PASS == SCAN_WHOLE ? a.q.seqs : a.slots), (unsigned)(a.groups * a.blocks_per_group));
+    CADNN_LAUNCH((scan_kernel<T, NS, L, PASS, FULL>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+// How a call is worked on, from its sizes alone.
+struct ScanPlan {
+    int few;                  // few tokens a sequence
+    int ns, lanes;            // states of a lane, lanes of a channel
+    int blocks_per_group;
+    int chunk;                // tokens of a piece; 0: whole sequences
+    int64_t slots;
+    size_t part_bytes, bytes;
+};
+
+ScanPlan plan_scan(const cadnn_scan_args& g) {
+    ScanPlan p{};
+    const int per = g.channels / g.groups;
+    p.ns = g.dstate <= 8 ? 8 : 16;
+    p.lanes = 1;
+    while (p.ns * p.lanes < g.dstate) p.lanes *= 2;
+    const int ch = 256 / p.lanes;
+    p.blocks_per_group = (per + ch - 1) / ch;
+    const int average = g.tokens / g.seqs;
+    p.few = average <= 4;
+    if (p.few) return p;
+    // Waves of one pass over whole sequences.  Two to a SIMD keep the vector units busy; below that, pieces are worked on
+    // side by side, at the price of a first pass for the states they start from (0.7 of a whole one).
+    const int64_t waves = (int64_t)g.seqs * g.groups * p.blocks_per_group * 4;
+    if (waves >= 2048 || average < 128) return p;
+    p.chunk = 512;
+    while (p.chunk > 64 && seq_slots(g.tokens, g.seqs, g.seq_start != nullptr, p.chunk) * g.groups * p.blocks_per_group * 4 < 2048) p.chunk /= 2;
+    p.slots = seq_slots(g.tokens, g.seqs, g.seq_start != nullptr, p.chunk);
+    p.part_bytes = (size_t)p.slots * g.channels * g.dstate * 4;
+    p.bytes = p.part_bytes + (size_t)p.slots * g.channels * 4;
+    return p;
+}
+
+template <typename T, int NS, int L, bool FULL>
+hipError_t launch_scan_passes(const SsArgs& a, hipStream_t s) {
+    if (!a.part) return launch_scan_pass<T, NS, L, SCAN_WHOLE, FULL>(a, s);
+    hipError_t e = launch_scan_pass<T, NS, L, SCAN_ENDS, FULL>(a, s);
+    if (e != hipSuccess) return e;
+    const int64_t per_seq = (int64_t)a.channels * a.dstate;
+    CADNN_LAUNCH(scan_join_kernel, dim3((unsigned)((per_seq + 255) / 256), (unsigned)a.q.seqs), dim3(256), 0, s, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    return launch_scan_pass<T, NS, L, SCAN_PIECES, FULL>(a, s);
+}
+
+template <typename T, int NS, int L>
+hipError_t launch_scan_lanes(const SsArgs& a, hipStream_t s) {
+    return a.dstate == NS * L ? launch_scan_passes<T, NS, L, true>(a, s) : launch_scan_passes<T, NS, L, false>(a, s);
+}
+
+template <typename T, int L>
+hipError_t launch_few_lanes(const SsArgs& a, hipStream_t s) {
+    const dim3 grid((unsigned)((a.channels + 256 / L - 1) / (256 / L)), (unsigned)a.q.seqs);
+    const bool vec = a.dstate % 4 == 0 && (uintptr_t)a.state % 16 == 0 && (uintptr_t)a.a % 16 == 0;
+    if (vec) CADNN_LAUNCH((scan_few_kernel<T, L, true>), grid, dim3(256), 0, s, a);
+    else CADNN_LAUNCH((scan_few_kernel<T, L, false>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_scan(const SsArgs& a, const ScanPlan& p, hipStream_t s) {
+    if (p.few) {
+        const int n = a.dstate;
+        return n <= 4 ? launch_few_lanes<T, 1>(a, s) : n <= 8 ? launch_few_lanes<T, 2>(a, s) : n <= 16 ? launch_few_lanes<T, 4>(a, s)
+             : n <= 32 ? launch_few_lanes<T, 8>(a, s) : n <= 64 ? launch_few_lanes<T, 16>(a, s) : n <= 128 ? launch_few_lanes<T, 32>(a, s)
+             : launch_few_lanes<T, 64>(a, s);
+    }
+    if (p.ns == 8) return launch_scan_lanes<T, 8, 1>(a, s);
+    switch (p.lanes) {
+        case 1: return launch_scan_lanes<T, 16, 1>(a, s);
+        case 2: return launch_scan_lanes<T, 16, 2>(a, s);
+        case 4: return launch_scan_lanes<T, 16, 4>(a, s);
+        case 8: return launch_scan_lanes<T, 16, 8>(a, s);
+        default: return launch_scan_lanes<T, 16, 16>(a, s);
+    }
+}
+
+cadnn_status check_scan(const char* who, const cadnn_scan_args* g) {
+    if (!g) return fail(CADNN_EINVAL, "%s: NULL arguments", who);
+    if (g->dtype != CADNN_F32 && g->dtype != CADNN_F16) return fail(CADNN_EINVAL, "%s: unknown dtype %d", who, (int)g->dtype);
+    cadnn_status st = check_sequences(who, g->tokens, g->seqs, g->seq_start);
+    if (st != CADNN_OK) return st;
+    if (g->channels <= 0 || g->dstate <= 0 || g->groups <= 0) return fail(CADNN_EINVAL, "%s: non-positive size", who);
+    if (g->channels % g->groups) return fail(CADNN_EINVAL, "%s: %d channels in %d groups", who, g->channels, g->groups);
+    if (g->dstate > kScanMaxStates) return fail(CADNN_EUNSUPPORTED, "%s: %d states a channel (at most %d are served)", who, g->dstate, kScanMaxStates);
+    if (g->channels > (1 << 20) || g->groups > 4096 || g->seqs > 65535) return fail(CADNN_EUNSUPPORTED, "%s: more than 2^20 channels, 4096 groups or 65535 sequences", who);
+    if ((int64_t)g->groups * plan_scan(*g).blocks_per_group > 65535) return fail(CADNN_EUNSUPPORTED, "%s: too many channels for one launch", who);
+    return CADNN_OK;
+}
+
+}  // namespace
+
+}  // namespace cadnn
+
+using namespace cadnn;
+
+extern "C" cadnn_status cadnn_selective_scan_workspace_bytes(const cadnn_scan_args* args, size_t* bytes) {
+    if (!bytes) return fail(CADNN_EINVAL, "cadnn_selective_scan_workspace_bytes: NULL pointer");
+    *bytes = 0;
+    cadnn_status st = check_scan("cadnn_selective_scan_workspace_bytes", args);
+    if (st != CADNN_OK) return st;
+    if (args->tokens > 0) *bytes = plan_scan(*args).bytes;
+    return CADNN_OK;
+}
+
+extern "C" cadnn_status cadnn_selective_scan(const cadnn_scan_args* args, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* who = "cadnn_selective_scan";
+    cadnn_status st = check_scan(who, args);
+    if (st != CADNN_OK) return st;
+    const cadnn_scan_args& g = *args;
+    if (g.tokens == 0) return CADNN_OK;
+    if (!g.x || !g.dt || !g.a || !g.b || !g.c || !g.y) return fail(CADNN_EINVAL, "%s: NULL tensor", who);
+    if (g.y == g.x || g.y == g.dt || g.y == g.b || g.y == g.c || g.y == g.z || g.y == (const void*)g.state)
+        return fail(CADNN_EINVAL, "%s: y must not overlap what is read", who);
+    if (g.x_stride < g.channels || g.dt_stride < g.channels || g.y_stride < g.channels || (g.z && g.z_stride < g.channels))
+        return fail(CADNN_EINVAL, "%s: rows overlap (a stride below the number of channels)", who);
+    if (g.b_stride < (int64_t)g.groups * g.dstate || g.c_stride < (int64_t)g.groups * g.dstate)
+        return fail(CADNN_EINVAL, "%s: rows overlap (a stride of b or c below groups * dstate)", who);
+    const uintptr_t e = g.dtype == CADNN_F16 ? 2 : 4;
+    if (((uintptr_t)g.x | (uintptr_t)g.dt | (uintptr_t)g.b | (uintptr_t)g.c | (uintptr_t)g.z | (uintptr_t)g.y) % e ||
+        ((uintptr_t)g.a | (uintptr_t)g.d | (uintptr_t)g.dt_bias | (uintptr_t)g.state | (uintptr_t)workspace) % 4)
+        return fail(CADNN_EINVAL, "%s: a misaligned pointer", who);
+    const ScanPlan p = plan_scan(g);
+    SsArgs a{};
+    a.x = g.x; a.dt = g.dt; a.b = g.b; a.c = g.c; a.z = g.z; a.y = g.y;
+    a.x_stride = g.x_stride; a.dt_stride = g.dt_stride; a.b_stride = g.b_stride; a.c_stride = g.c_stride; a.z_stride = g.z_stride; a.y_stride = g.y_stride;
+    a.a = g.a; a.d = g.d; a.dt_bias = g.dt_bias; a.state = g.state;
+    a.q = Sequences{g.seq_start, g.tokens, g.seqs};
+    a.channels = g.channels; a.dstate = g.dstate; a.groups = g.groups; a.per = g.channels / g.groups; a.softplus = g.softplus ? 1 : 0;
+    a.blocks_per_group = p.blocks_per_group;
+    if (p.chunk > 0 && workspace && workspace_bytes >= p.bytes) {
+        a.chunk = p.chunk;
+        a.slots = p.slots;
+        a.part = (float*)workspace;
+        a.span = (float*)((char*)workspace + p.part_bytes);
+    }
+    CADNN_HIP(g.dtype == CADNN_F16 ? launch_scan<_Float16>(a, p, (hipStream_t)stream) : launch_scan<float>(a, p, (hipStream_t)stream));
+    return CADNN_OK;
+}
