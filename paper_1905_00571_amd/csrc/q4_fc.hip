@@ -98,15 +98,16 @@ __device__ __forceinline__ q4_f4 q4_scales(const _Float16* p) {
 }
 __device__ __forceinline__ q4_f4 q4_scales(const float* p) { return *(const q4_f4*)p; }
 
-// Eight activations from input i0 on; what lies behind the row's end, or in no row, is zero.
-template <typename T, bool VEC>
+// Eight activations from input i0 on; what lies behind the row's end, or in no row, is zero.  (Rows need not start at
+// multiples of 16 bytes: the loads are as wide for any alignment.)
+template <typename T>
 __device__ __forceinline__ void q4_load_x(const T* row, int i0, int cin, bool real, T (&v)[8]) {
-    if (VEC && i0 + 8 <= cin) {
-        typedef T V __attribute__((ext_vector_type(16 / sizeof(T))));
-        constexpr int N = 16 / (int)sizeof(T);
+    constexpr int N = 16 / (int)sizeof(T);
+    typedef T V __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+    if (i0 + 8 <= cin) {
 #pragma unroll
         for (int k = 0; k < 8; k += N) {
-            V p = {};
+            V p = (V)(T)0.0f;
             if (real) p = *(const V*)(row + i0 + k);
 #pragma unroll
             for (int e = 0; e < N; ++e) v[k + e] = p[e];
@@ -138,7 +139,7 @@ __device__ __forceinline__ void q4_store(const Q4Args& a, int token, int o0, q4_
 // Few tokens: the weights are read once and bound the kernel.  A workgroup owns 16 * RT filters and 16 * NT tokens and its
 // waves split the inputs, block by block in turn, so that even one tile of filters is read by eight waves; their sums meet
 // in LDS and are added in the waves' order.
-template <typename T, int GP, int RT, int NT, bool VEC>
+template <typename T, int GP, int RT, int NT>
 __global__ __launch_bounds__(512) void q4_few_kernel(const Q4Args a) {
     typedef Q4Frag<T> F;
     extern __shared__ __attribute__((aligned(16))) char q4_smem[];
@@ -175,7 +176,7 @@ __global__ __launch_bounds__(512) void q4_few_kernel(const Q4Args a) {
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 T v[8];
-                q4_load_x<T, VEC>(rows[t], b * 128 + s * 32 + g * 8, a.cin, real[t], v);
+                q4_load_x<T>(rows[t], b * 128 + s * 32 + g * 8, a.cin, real[t], v);
                 F::parts(v, xf[t][s]);
             }
 #pragma unroll
@@ -211,24 +212,200 @@ __global__ __launch_bounds__(512) void q4_few_kernel(const Q4Args a) {
 }
 
 template <typename T, int GP, int RT, int NT>
-hipError_t launch_few(const Q4Args& a, bool vec, hipStream_t s) {
+hipError_t launch_few(const Q4Args& a, hipStream_t s) {
     const int tiles = (a.cout + 15) / 16;
     const int waves = a.blocks >= 8 ? 8 : a.blocks;
     const dim3 grid((unsigned)((tiles + RT - 1) / RT), (unsigned)((a.n + 16 * NT - 1) / (16 * NT)));
     const size_t lds = (size_t)waves * RT * NT * 64 * sizeof(q4_f4);
-    if (vec) CADNN_LAUNCH((q4_few_kernel<T, GP, RT, NT, true>), grid, dim3(64u * waves), lds, s, a);
-    else CADNN_LAUNCH((q4_few_kernel<T, GP, RT, NT, false>), grid, dim3(64u * waves), lds, s, a);
+    CADNN_LAUNCH((q4_few_kernel<T, GP, RT, NT>), grid, dim3(64u * waves), lds, s, a);
+    return hipGetLastError();
+}
+
+// Many tokens: the matrix cores bound the kernel.  A workgroup owns 256 filters and BN tokens; each of its four waves owns
+// 64 filters, whose codes it loads straight into the lanes that need them and expands in registers (no other wave needs
+// them), and all BN tokens, whose activations are staged in LDS, 128 inputs at a time.  The 16-byte pieces of a token's row
+// lie in LDS at their place exclusive-or the token's number, so that the sixteen lanes that read the same piece of sixteen
+// tokens meet all banks.  A wave's sums of 64 inputs (two steps; one with groups of 32) start from zero in the first matrix
+// instruction and are multiplied by the scale into the fp32 accumulators: per 64 inputs and 64 x 128 outputs of a wave that
+// is 512 + 288 cycles of vector work beside 1024 of matrix work.
+template <typename T, int GP, int BN, bool DIRECT>
+__global__ __launch_bounds__(256, 2) void q4_tile_kernel(const Q4Args a) {
+    typedef Q4Frag<T> F;
+    constexpr int P = F::kParts, CT = BN / 16, BUF = BN * 256 * P;         // bytes of a staged block
+    constexpr int SUB = GP == 4 ? 2 : 1;                                    // scales per 64 inputs
+    extern __shared__ __attribute__((aligned(16))) char q4_smem[];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int j = lane & 15, g = lane >> 4;
+    const int tiles = (a.cout + 15) / 16;
+    const int tile0 = (int)blockIdx.x * 16 + wave * 4;
+    const int token0 = (int)blockIdx.y * BN;
+    const int rows_here = min(BN, a.n - token0);
+    const T* x0 = (const T*)a.x + (int64_t)token0 * a.x_stride;
+    // what a thread stages: pieces of 8 inputs (16 bytes in fp16) of the block's BN x 16
+    constexpr int PIECES = BN * 16 / 256;
+    auto lds_at = [&](int buf, int part, int row, int piece) {
+        return (uint32_t)(buf * BUF + part * BN * 256 + row * 256 + ((piece ^ (row & 15)) << 4));
+    };
+    T held[DIRECT ? 1 : PIECES][8];
+    auto fetch = [&](int b) {                 // into registers
+        if constexpr (!DIRECT) {
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) {
+                const int i = k * 256 + tid, row = i >> 4, piece = i & 15;
+                q4_load_x<T>(x0 + (int64_t)(row < rows_here ? row : 0) * a.x_stride, b * 128 + piece * 8, a.cin, row < rows_here, held[k]);
+            }
+        }
+    };
+    auto put = [&](int buf) {                 // ... and from there to LDS
+        if constexpr (!DIRECT) {
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) {
+                const int i = k * 256 + tid, row = i >> 4, piece = i & 15;
+                typename F::V parts[P];
+                F::parts(held[k], parts);
+#pragma unroll
+                for (int p = 0; p < P; ++p) *(typename F::V*)(q4_smem + lds_at(buf, p, row, piece)) = parts[p];
+            }
+        }
+    };
+    __amdgpu_buffer_rsrc_t rsrc;
+    uint32_t voff[DIRECT ? PIECES : 1];
+    if constexpr (DIRECT) {
+        const uint32_t span = (uint32_t)((rows_here - 1) * a.x_stride + a.cin) * 2u;
+        rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)x0, 0, span, 0x00020000);
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            const int i = k * 256 + tid, row = i >> 4, piece = (i & 15) ^ (row & 15);
+            voff[k] = row < rows_here ? (uint32_t)(row * a.x_stride + piece * 8) * 2u : 0xffffffffu;
+        }
+    }
+    auto copy = [&](int b, int buf) {         // straight to LDS: a wave's 64 pieces follow each other there, so the pieces are permuted as they are read
+        if constexpr (DIRECT) {
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) {
+                const int i = k * 256 + tid, row = i >> 4, piece = (i & 15) ^ (row & 15);
+                const bool in = b * 128 + piece * 8 < a.cin && voff[k] != 0xffffffffu;
+                const uint32_t off = in ? voff[k] + (uint32_t)b * 256u : 0xfffffff0u;       // (behind the buffer's end: zero)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(q4_smem + buf * BUF + (k * 256 + wave * 64) * 16),
+                                                         16, off, 0, 0, 0);
+            }
+        }
+    };
+    q4_f4 acc[4][CT];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) acc[r][c] = (q4_f4){0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t* code_at[4];
+    const T* scale_at[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int tile = min(tile0 + r, tiles - 1);
+        code_at[r] = a.codes + (int64_t)tile * a.blocks * 256 + lane * 4;
+        scale_at[r] = (const T*)a.scales + (int64_t)tile * a.blocks * GP * 16 + 4 * g;
+    }
+    q4_u4 w[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) w[r] = *(const q4_u4*)code_at[r];
+    if constexpr (DIRECT) {
+        copy(0, 0);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    } else {
+        fetch(0);
+        put(0);
+    }
+    __syncthreads();
+    int buf = 0;
+    for (int b = 0; b < a.blocks; ++b) {
+        const int next = min(b + 1, a.blocks - 1);
+        if constexpr (DIRECT) copy(next, buf ^ 1);
+        else fetch(next);
+        q4_u4 wn[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) wn[r] = *(const q4_u4*)(code_at[r] + (int64_t)next * 256);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            q4_f4 sc[4][SUB];
+            typename F::V af[4][2];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                for (int q = 0; q < SUB; ++q) {
+                    const int group = GP == 1 ? 0 : GP == 2 ? half : half * 2 + q;
+                    sc[r][q] = q4_scales(scale_at[r] + ((int64_t)b * GP + group) * 16);
+                }
+                af[r][0] = F::codes(w[r][half * 2]);
+                af[r][1] = F::codes(w[r][half * 2 + 1]);
+            }
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                typename F::V xf[2][P];
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+                        xf[s][p] = *(const typename F::V*)(q4_smem + lds_at(DIRECT ? buf : 0, p, c * 16 + j, (half * 2 + s) * 4 + g));
+                q4_f4 sum[4];
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                    for (int p = P - 1; p >= 0; --p)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            sum[r] = F::mul(af[r][s], xf[s][p], p == P - 1 && (s == 0 || SUB == 2) ? (q4_f4){0.0f, 0.0f, 0.0f, 0.0f} : sum[r]);
+                    if (s == 1 || SUB == 2) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[r][c][e] = fmaf(sc[r][SUB == 2 ? s : 0][e], sum[r][e], acc[r][c][e]);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) w[r] = wn[r];
+        // (what a wave copies has arrived before it meets the others)
+        if constexpr (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if constexpr (DIRECT) buf ^= 1;
+        else {
+            put(0);
+            __syncthreads();
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) q4_store<T>(a, token0 + c * 16 + j, (tile0 + r) * 16 + 4 * g, acc[r][c]);
+}
+
+template <typename T, int GP, int BN, bool DIRECT>
+hipError_t launch_tile(const Q4Args& a, hipStream_t s) {
+    constexpr int lds = (DIRECT ? 2 : 1) * BN * 256 * Q4Frag<T>::kParts;
+    static const hipError_t attr = hipFuncSetAttribute((const void*)q4_tile_kernel<T, GP, BN, DIRECT>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (attr != hipSuccess) return attr;
+    const dim3 grid((unsigned)((a.cout + 255) / 256), (unsigned)((a.n + BN - 1) / BN));
+    CADNN_LAUNCH((q4_tile_kernel<T, GP, BN, DIRECT>), grid, dim3(256), lds, s, a);
     return hipGetLastError();
 }
 
 template <typename T, int GP>
-hipError_t launch_q4(const Q4Args& a, bool vec, hipStream_t s) {
-    return launch_few<T, GP, 1, 1>(a, vec, s);
+hipError_t launch_q4(const Q4Args& a, hipStream_t s) {
+    if (a.n > 64) {
+        if constexpr (sizeof(T) == 2) {
+            // (32-bit offsets from the first token of a tile on)
+            const bool direct = (uintptr_t)a.x % 16 == 0 && a.x_stride % 8 == 0 && a.cin % 8 == 0 && a.x_stride < (1 << 22);
+            return direct ? launch_tile<T, GP, 128, true>(a, s) : launch_tile<T, GP, 64, false>(a, s);
+        } else {
+            return launch_tile<T, GP, 64, false>(a, s);
+        }
+    }
+    return launch_few<T, GP, 1, 1>(a, s);
 }
 
 template <typename T>
-hipError_t launch_q4_group(const Q4Args& a, int group, bool vec, hipStream_t s) {
-    return group == 128 ? launch_q4<T, 1>(a, vec, s) : group == 64 ? launch_q4<T, 2>(a, vec, s) : launch_q4<T, 4>(a, vec, s);
+hipError_t launch_q4_group(const Q4Args& a, int group, hipStream_t s) {
+    return group == 128 ? launch_q4<T, 1>(a, s) : group == 64 ? launch_q4<T, 2>(a, s) : launch_q4<T, 4>(a, s);
 }
 
 }  // namespace
@@ -244,9 +421,8 @@ cadnn_status launch_q4_fc(const cadnn_q4_weights* w, const void* x, int64_t x_st
         a.x = (const char*)x + (size_t)n0 * x_stride * e; a.y = (char*)y + (size_t)n0 * y_stride * e;
         a.x_stride = x_stride; a.y_stride = y_stride;
         a.n = std::min(step, n - n0); a.cin = w->cin; a.cout = w->cout; a.blocks = (w->cin + kQ4Block - 1) / kQ4Block; a.act = act;
-        a.y_vec = (uintptr_t)y % (4 * e) == 0 && y_stride % 4 == 0;
-        const bool vec = (uintptr_t)x % 16 == 0 && (x_stride * (int64_t)e) % 16 == 0;
-        CADNN_HIP(w->dtype == CADNN_F16 ? launch_q4_group<_Float16>(a, w->group, vec, s) : launch_q4_group<float>(a, w->group, vec, s));
+        a.y_vec = (uintptr_t)a.y % (4 * e) == 0 && y_stride % 4 == 0;
+        CADNN_HIP(w->dtype == CADNN_F16 ? launch_q4_group<_Float16>(a, w->group, s) : launch_q4_group<float>(a, w->group, s));
     }
     return CADNN_OK;
 }
