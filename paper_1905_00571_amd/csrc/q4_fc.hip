@@ -211,6 +211,117 @@ __global__ __launch_bounds__(512) void q4_few_kernel(const Q4Args a) {
     }
 }
 
+// As many tokens as one matrix instruction has columns: 16 in fp16, five in fp32, where the three parts of a token take three
+// columns and one instruction serves all of them.  The workgroup brings the activations of a chunk (one block for every
+// wave) into LDS, each element read, and cut apart, once, while the matrix instructions work on the chunk before, and a wave's
+// codes and scales are fetched D chunks ahead.  us at 8192 -> 8192, groups of 128, one token: fp16 10.6, fp32 12.3, where the kernel above
+// takes 14.2 and 19.6; the 35 MB are 6.4 us at the rate of a large copy.
+template <typename T, int GP, int RT, int HELD>
+__global__ __launch_bounds__(512) void q4_columns_kernel(const Q4Args a) {
+    typedef Q4Frag<T> F;
+    constexpr int P = F::kParts;
+    constexpr int D = RT * GP * (int)sizeof(T) >= 16 ? 2 : 4;
+    extern __shared__ __attribute__((aligned(16))) char q4_smem[];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = (int)blockDim.x >> 6;
+    const int j = lane & 15, g = lane >> 4;
+    const int tile0 = (int)blockIdx.x * RT, tiles = (a.cout + 15) / 16;
+    const uint32_t buf_bytes = (uint32_t)waves * 4096u;        // [block][16 columns][128 inputs], pieces of 16 bytes placed as below
+    auto at = [&](uint32_t buf, int block, int col, int piece) { return q4_smem + buf * buf_bytes + block * 4096 + col * 256 + ((piece ^ col) << 4); };
+    for (uint32_t i = (uint32_t)tid * 16u; i < 2 * buf_bytes; i += blockDim.x * 16u) *(q4_u4*)(q4_smem + i) = (q4_u4){0u, 0u, 0u, 0u};
+    __syncthreads();
+    const T* x = (const T*)a.x;
+    const int per_token = 16 * waves;
+    T held[HELD][8];                              // HELD pieces of a chunk are a thread's: a quarter of the tokens
+    auto fetch = [&](int chunk) {
+        const bool whole = (chunk + 1) * waves * 128 <= a.cin;       // (no row ends in the chunk: one wide load a piece)
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            const int i = k * 64 * waves + tid, token = i / per_token, r = i - token * per_token;
+            if (token < a.n) q4_load_x<T>(x + (int64_t)token * a.x_stride, chunk * waves * 128 + r * 8, whole ? 1 << 30 : a.cin, true, held[k]);
+        }
+    };
+    auto put = [&](uint32_t buf) {
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            const int i = k * 64 * waves + tid, token = i / per_token, r = i - token * per_token;
+            if (token < a.n) {
+                typename F::V parts[P];
+                F::parts(held[k], parts);
+#pragma unroll
+                for (int p = 0; p < P; ++p) *(typename F::V*)at(buf, r >> 4, token * P + p, r & 15) = parts[p];
+            }
+        }
+    };
+    q4_u4 w[D][RT];
+    q4_f4 sc[D][RT][GP], acc[RT];
+    auto codes = [&](int slot, int chunk) {
+        const int b = min(chunk * waves + wave, a.blocks - 1);      // (behind the last block the activations are zero)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const int64_t block = (int64_t)min(tile0 + r, tiles - 1) * a.blocks + b;
+            w[slot][r] = *(const q4_u4*)(a.codes + block * 256 + lane * 4);
+#pragma unroll
+            for (int p = 0; p < GP; ++p) sc[slot][r][p] = q4_scales((const T*)a.scales + (block * GP + p) * 16 + 4 * g);
+        }
+    };
+#pragma unroll
+    for (int d = 0; d < D; ++d) codes(d, d);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) acc[r] = (q4_f4){0.0f, 0.0f, 0.0f, 0.0f};
+    fetch(0);
+    put(0);
+    __syncthreads();
+    const int chunks = (a.blocks + waves - 1) / waves;
+    uint32_t buf = 0;
+    for (int c0 = 0; c0 < chunks; c0 += D) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            const int c = c0 + d;
+            if (c < chunks) {
+                if (c + 1 < chunks) fetch(c + 1);
+                q4_f4 sum[RT];
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const typename F::V xf = *(const typename F::V*)at(buf, wave, j, s * 4 + g);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        sum[r] = F::mul(F::codes(w[d][r][s]), xf, s % (4 / GP) == 0 ? (q4_f4){0.0f, 0.0f, 0.0f, 0.0f} : sum[r]);
+                        if ((s + 1) % (4 / GP) == 0) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[r][e] = fmaf(sc[d][r][s / (4 / GP)][e], sum[r][e], acc[r][e]);
+                        }
+                    }
+                }
+                codes(d, c + D);
+                if (c + 1 < chunks) put(buf ^ 1);
+                __syncthreads();
+                buf ^= 1;
+            }
+        }
+    }
+    q4_f4* part = (q4_f4*)q4_smem;       // [wave][r][lane]
+#pragma unroll
+    for (int r = 0; r < RT; ++r) part[(wave * RT + r) * 64 + lane] = acc[r];
+    __syncthreads();
+    for (int i = tid; i < RT * 4 * a.n; i += (int)blockDim.x) {
+        const int r = i & (RT - 1), gg = (i / RT) & 3, token = i / (RT * 4);
+        q4_f4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k = 0; k < waves; ++k)
+            for (int p = P - 1; p >= 0; --p) v += part[(k * RT + r) * 64 + gg * 16 + token * P + p];
+        q4_store<T>(a, token, (tile0 + r) * 16 + 4 * gg, v);
+    }
+}
+
+template <typename T, int GP, int RT>
+hipError_t launch_columns(const Q4Args& a, hipStream_t s) {
+    const int tiles = (a.cout + 15) / 16, waves = a.blocks >= 8 ? 8 : a.blocks;
+    const size_t lds = (size_t)waves * 8192;
+    const dim3 grid((unsigned)((tiles + RT - 1) / RT));
+    if (a.n <= 4) CADNN_LAUNCH((q4_columns_kernel<T, GP, RT, 1>), grid, dim3(64u * waves), lds, s, a);
+    else CADNN_LAUNCH((q4_columns_kernel<T, GP, RT, Q4Frag<T>::kParts == 3 ? 2 : 4>), grid, dim3(64u * waves), lds, s, a);
+    return hipGetLastError();
+}
+
 template <typename T, int GP, int RT, int NT>
 hipError_t launch_few(const Q4Args& a, hipStream_t s) {
     const int tiles = (a.cout + 15) / 16;
@@ -221,23 +332,29 @@ hipError_t launch_few(const Q4Args& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Many tokens: the matrix cores bound the kernel.  A workgroup owns 256 filters and BN tokens; each of its four waves owns
-// 64 filters, whose codes it loads straight into the lanes that need them and expands in registers (no other wave needs
+// Many tokens: the matrix cores bound the kernel.  A workgroup owns 64 * RW filters and BN tokens; each of its four waves owns
+// 16 * RW filters, whose codes it loads straight into the lanes that need them and expands in registers (no other wave needs
 // them), and all BN tokens, whose activations are staged in LDS, 128 inputs at a time.  The 16-byte pieces of a token's row
 // lie in LDS at their place exclusive-or the token's number, so that the sixteen lanes that read the same piece of sixteen
-// tokens meet all banks.  A wave's sums of 64 inputs (two steps; one with groups of 32) start from zero in the first matrix
-// instruction and are multiplied by the scale into the fp32 accumulators: per 64 inputs and 64 x 128 outputs of a wave that
-// is 512 + 288 cycles of vector work beside 1024 of matrix work.
-template <typename T, int GP, int BN, bool DIRECT>
-__global__ __launch_bounds__(256, 2) void q4_tile_kernel(const Q4Args a) {
+// tokens meet all banks.  KS steps of 32 inputs are expanded at a time; their sums start from zero in the first matrix
+// instruction and are multiplied by the group's scale into the fp32 accumulators, which for groups of 32 is as much vector
+// work as there is matrix work.  (With the scale multiplied into the codes, rounded to fp16, 2048 tokens through 4096 -> 8192 took 128 us for
+// any group, where this takes 145, 155 and 185 for groups of 128, 64 and 32; the library's fp16 product takes 114.)  WK = 2: two
+// times four waves take the blocks in turn and add up, where there are too few workgroups to wait for each other's loads.
+// DIRECT (fp16): activations go straight to LDS, into the second of two buffers, else through registers.
+template <typename T, int GP, int RW, int BN, int KS, int WK, bool DIRECT>
+__global__ __launch_bounds__(256 * WK, 2) void q4_tile_kernel(const Q4Args a) {
     typedef Q4Frag<T> F;
     constexpr int P = F::kParts, CT = BN / 16, BUF = BN * 256 * P;         // bytes of a staged block
-    constexpr int SUB = GP == 4 ? 2 : 1;                                    // scales per 64 inputs
+    constexpr int NBUF = DIRECT ? 2 : 1;
+    constexpr int PER = 4 / GP < KS ? 4 / GP : KS;                          // steps that share a scale, in a phase
     extern __shared__ __attribute__((aligned(16))) char q4_smem[];
-    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = (int)threadIdx.x & 255, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wk = WK == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8);
+    char* smem = q4_smem + wk * (NBUF * BUF);
     const int j = lane & 15, g = lane >> 4;
     const int tiles = (a.cout + 15) / 16;
-    const int tile0 = (int)blockIdx.x * 16 + wave * 4;
+    const int tile0 = ((int)blockIdx.x * 4 + wave) * RW;
     const int token0 = (int)blockIdx.y * BN;
     const int rows_here = min(BN, a.n - token0);
     const T* x0 = (const T*)a.x + (int64_t)token0 * a.x_stride;
@@ -264,7 +381,7 @@ __global__ __launch_bounds__(256, 2) void q4_tile_kernel(const Q4Args a) {
                 typename F::V parts[P];
                 F::parts(held[k], parts);
 #pragma unroll
-                for (int p = 0; p < P; ++p) *(typename F::V*)(q4_smem + lds_at(buf, p, row, piece)) = parts[p];
+                for (int p = 0; p < P; ++p) *(typename F::V*)(smem + lds_at(buf, p, row, piece)) = parts[p];
             }
         }
     };
@@ -283,123 +400,172 @@ __global__ __launch_bounds__(256, 2) void q4_tile_kernel(const Q4Args a) {
         if constexpr (DIRECT) {
 #pragma unroll
             for (int k = 0; k < PIECES; ++k) {
-                const int i = k * 256 + tid, row = i >> 4, piece = (i & 15) ^ (row & 15);
+                const int piece = (tid & 15) ^ (((k * 256 + tid) >> 4) & 15);
                 const bool in = b * 128 + piece * 8 < a.cin && voff[k] != 0xffffffffu;
                 const uint32_t off = in ? voff[k] + (uint32_t)b * 256u : 0xfffffff0u;       // (behind the buffer's end: zero)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(q4_smem + buf * BUF + (k * 256 + wave * 64) * 16),
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(smem + buf * BUF + (k * 256 + wave * 64) * 16),
                                                          16, off, 0, 0, 0);
             }
         }
     };
-    q4_f4 acc[4][CT];
+    q4_f4 acc[RW][CT];
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < RW; ++r)
 #pragma unroll
         for (int c = 0; c < CT; ++c) acc[r][c] = (q4_f4){0.0f, 0.0f, 0.0f, 0.0f};
-    const uint32_t* code_at[4];
-    const T* scale_at[4];
+    const uint32_t* code_at[RW];
+    const T* scale_at[RW];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < RW; ++r) {
         const int tile = min(tile0 + r, tiles - 1);
         code_at[r] = a.codes + (int64_t)tile * a.blocks * 256 + lane * 4;
         scale_at[r] = (const T*)a.scales + (int64_t)tile * a.blocks * GP * 16 + 4 * g;
     }
-    q4_u4 w[4];
+    const int steps = (a.blocks + WK - 1) / WK;
+    q4_u4 w[RW];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) w[r] = *(const q4_u4*)code_at[r];
+    for (int r = 0; r < RW; ++r) w[r] = *(const q4_u4*)(code_at[r] + (int64_t)min(wk, a.blocks - 1) * 256);
     if constexpr (DIRECT) {
-        copy(0, 0);
+        copy(wk, 0);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     } else {
-        fetch(0);
+        fetch(wk);
         put(0);
     }
     __syncthreads();
     int buf = 0;
-    for (int b = 0; b < a.blocks; ++b) {
-        const int next = min(b + 1, a.blocks - 1);
-        if constexpr (DIRECT) copy(next, buf ^ 1);
-        else fetch(next);
-        q4_u4 wn[4];
+    for (int i = 0; i < steps; ++i) {
+        const int b = i * WK + wk, next = min(b + WK, a.blocks - 1);
+        const bool more = i + 1 < steps;
+        if (more) {
+            if constexpr (DIRECT) copy(b + WK, buf ^ 1);
+            else fetch(b + WK);
+        }
+        q4_u4 wn[RW];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) wn[r] = *(const q4_u4*)(code_at[r] + (int64_t)next * 256);
+        for (int r = 0; r < RW; ++r) wn[r] = *(const q4_u4*)(code_at[r] + (int64_t)next * 256);
+        if (WK == 1 || b < a.blocks) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            q4_f4 sc[4][SUB];
-            typename F::V af[4][2];
+            for (int ph = 0; ph < 4 / KS; ++ph) {
+                q4_f4 sc[RW][KS / PER];
+                typename F::V af[RW][KS];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
+                for (int r = 0; r < RW; ++r) {
 #pragma unroll
-                for (int q = 0; q < SUB; ++q) {
-                    const int group = GP == 1 ? 0 : GP == 2 ? half : half * 2 + q;
-                    sc[r][q] = q4_scales(scale_at[r] + ((int64_t)b * GP + group) * 16);
+                    for (int q = 0; q < KS / PER; ++q) sc[r][q] = q4_scales(scale_at[r] + ((int64_t)b * GP + (ph * KS + q * PER) * GP / 4) * 16);
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) af[r][s] = F::codes(w[r][ph * KS + s]);
                 }
-                af[r][0] = F::codes(w[r][half * 2]);
-                af[r][1] = F::codes(w[r][half * 2 + 1]);
-            }
 #pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                typename F::V xf[2][P];
+                for (int c = 0; c < CT; ++c) {
+                    typename F::V xf[KS][P];
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
+                    for (int s = 0; s < KS; ++s)
 #pragma unroll
-                    for (int p = 0; p < P; ++p)
-                        xf[s][p] = *(const typename F::V*)(q4_smem + lds_at(DIRECT ? buf : 0, p, c * 16 + j, (half * 2 + s) * 4 + g));
-                q4_f4 sum[4];
+                        for (int p = 0; p < P; ++p)
+                            xf[s][p] = *(const typename F::V*)(smem + lds_at(buf, p, c * 16 + j, (ph * KS + s) * 4 + g));
+                    q4_f4 sum[RW];
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
+                    for (int s = 0; s < KS; ++s) {
 #pragma unroll
-                    for (int p = P - 1; p >= 0; --p)
+                        for (int p = P - 1; p >= 0; --p)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            sum[r] = F::mul(af[r][s], xf[s][p], p == P - 1 && (s == 0 || SUB == 2) ? (q4_f4){0.0f, 0.0f, 0.0f, 0.0f} : sum[r]);
-                    if (s == 1 || SUB == 2) {
+                            for (int r = 0; r < RW; ++r)
+                                sum[r] = F::mul(af[r][s], xf[s][p], p == P - 1 && s % PER == 0 ? (q4_f4){0.0f, 0.0f, 0.0f, 0.0f} : sum[r]);
+                        if ((s + 1) % PER == 0) {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
+                            for (int r = 0; r < RW; ++r)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[r][c][e] = fmaf(sc[r][SUB == 2 ? s : 0][e], sum[r][e], acc[r][c][e]);
+                                for (int e = 0; e < 4; ++e) acc[r][c][e] = fmaf(sc[r][s / PER][e], sum[r][e], acc[r][c][e]);
+                        }
                     }
                 }
             }
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) w[r] = wn[r];
+        for (int r = 0; r < RW; ++r) w[r] = wn[r];
         // (what a wave copies has arrived before it meets the others)
         if constexpr (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if constexpr (DIRECT) buf ^= 1;
-        else {
+        else if (more) {
             put(0);
             __syncthreads();
         }
     }
+    if constexpr (WK == 2) {
+        q4_f4* part = (q4_f4*)q4_smem;
+        if (wk == 1) {
+#pragma unroll
+            for (int r = 0; r < RW; ++r)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) part[(r * CT + c) * 256 + tid] = acc[r][c];
+        }
+        __syncthreads();
+        if (wk == 1) return;
+#pragma unroll
+        for (int r = 0; r < RW; ++r)
+#pragma unroll
+            for (int c = 0; c < CT; ++c) acc[r][c] += part[(r * CT + c) * 256 + tid];
+    }
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) q4_store<T>(a, token0 + c * 16 + j, (tile0 + r) * 16 + 4 * g, acc[r][c]);
+        for (int r = 0; r < RW; ++r) q4_store<T>(a, token0 + c * 16 + j, (tile0 + r) * 16 + 4 * g, acc[r][c]);
 }
 
-template <typename T, int GP, int BN, bool DIRECT>
+template <typename T, int GP, int RW, int BN, int KS, int WK, bool DIRECT>
 hipError_t launch_tile(const Q4Args& a, hipStream_t s) {
-    constexpr int lds = (DIRECT ? 2 : 1) * BN * 256 * Q4Frag<T>::kParts;
-    static const hipError_t attr = hipFuncSetAttribute((const void*)q4_tile_kernel<T, GP, BN, DIRECT>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    constexpr int staged = (DIRECT ? 2 : 1) * BN * 256 * Q4Frag<T>::kParts * WK, joined = WK == 2 ? 64 * RW * BN * 4 : 0;
+    constexpr int lds = staged > joined ? staged : joined;
+    static const hipError_t attr = hipFuncSetAttribute((const void*)q4_tile_kernel<T, GP, RW, BN, KS, WK, DIRECT>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (attr != hipSuccess) return attr;
-    const dim3 grid((unsigned)((a.cout + 255) / 256), (unsigned)((a.n + BN - 1) / BN));
-    CADNN_LAUNCH((q4_tile_kernel<T, GP, BN, DIRECT>), grid, dim3(256), lds, s, a);
+    const dim3 grid((unsigned)((a.cout + 64 * RW - 1) / (64 * RW)), (unsigned)((a.n + BN - 1) / BN));
+    CADNN_LAUNCH((q4_tile_kernel<T, GP, RW, BN, KS, WK, DIRECT>), grid, dim3(256 * WK), lds, s, a);
     return hipGetLastError();
 }
 
+// Which kernel: the largest tile that still gives every compute unit a workgroup (large tiles read and expand less, but a
+// workgroup alone on its unit waits out every latency); below that, and for few tokens, the kernels that split the inputs
+// over a workgroup's waves.  us on random data, 4096 -> 4096, groups of 128, fp16: 64 tokens 11.5 (few), 12.8 (64 x 32 tiles);
+// 128 tokens 17.1, 13.6; 512 tokens 29.7 (64 x 32), 25.2 (128 x 64), 53 (128 x 128); 2048 tokens 78 (128 x 64), 76 (128 x 128), and with
+// groups of 32 130 and 98.  fp32, 512 tokens: 82 (few), 59 (128 x 32), 55 (256 x 32), 94 (256 x 64); 2048 tokens: 216 (256 x 32), 200 (256 x 64).
 template <typename T, int GP>
 hipError_t launch_q4(const Q4Args& a, hipStream_t s) {
-    if (a.n > 64) {
+    auto fills = [&](int filters, int tokens, int workgroups) {
+        return (int64_t)((a.cout + filters - 1) / filters) * ((a.n + tokens - 1) / tokens) >= workgroups;
+    };
+    if (a.n > 32) {
         if constexpr (sizeof(T) == 2) {
-            // (32-bit offsets from the first token of a tile on)
+            // straight to LDS: whole pieces of eight, and 32-bit offsets from the first token of a tile on
             const bool direct = (uintptr_t)a.x % 16 == 0 && a.x_stride % 8 == 0 && a.cin % 8 == 0 && a.x_stride < (1 << 22);
-            return direct ? launch_tile<T, GP, 128, true>(a, s) : launch_tile<T, GP, 64, false>(a, s);
+            if (direct) {
+                if (fills(128, 128, 512)) return launch_tile<T, GP, 2, 128, GP == 1 ? 4 : 2, 1, true>(a, s);
+                if (fills(128, 64, 256)) return launch_tile<T, GP, 2, 64, 4, 2, true>(a, s);
+                if (fills(64, 32, 256)) return launch_tile<T, GP, 1, 32, 4, 2, true>(a, s);
+            } else {
+                if (fills(128, 64, 1024)) return launch_tile<T, GP, 2, 64, 4, 1, false>(a, s);
+                if (fills(128, 64, 256)) return launch_tile<T, GP, 2, 64, 4, 2, false>(a, s);
+                if (fills(64, 32, 256)) return launch_tile<T, GP, 1, 32, 4, 2, false>(a, s);
+            }
         } else {
-            return launch_tile<T, GP, 64, false>(a, s);
+            if (fills(256, 64, 256)) return launch_tile<T, GP, 4, 64, 2, 2, false>(a, s);
+            if (fills(256, 32, 256)) return launch_tile<T, GP, 4, 32, 4, 2, false>(a, s);
+            if (fills(128, 32, 256)) return launch_tile<T, GP, 2, 32, 4, 2, false>(a, s);
+            if (fills(64, 32, 256)) return launch_few<T, GP, 4, 2>(a, s);
         }
     }
+    // Staged activations pay from rows of some length on (one token, 512 -> 512: fp16 3.5 staged, 2.9 not; 4096 -> 4096: 5.0, 5.9), two
+    // tiles of filters to a wave where it has activations to cut apart (fp32, 5 tokens, 8192 -> 8192: 17.1 one, 15.3 two).
+    const bool two = fills(32, 16, 256) && a.blocks > 8;
+    if constexpr (sizeof(T) == 2) {
+        if (a.blocks > 16 && a.n <= 16) return launch_columns<T, GP, 1>(a, s);
+    } else {
+        if (a.blocks > 8 && a.n <= 5) return two ? launch_columns<T, GP, 2>(a, s) : launch_columns<T, GP, 1>(a, s);
+    }
+    if (a.n <= 16) return two ? launch_few<T, GP, 2, 1>(a, s) : launch_few<T, GP, 1, 1>(a, s);
+    if (fills(64, 16, 256)) return launch_few<T, GP, 4, 1>(a, s);
+    if (fills(32, 16, 256)) return launch_few<T, GP, 2, 1>(a, s);
     return launch_few<T, GP, 1, 1>(a, s);
 }
 
