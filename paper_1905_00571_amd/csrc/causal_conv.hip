@@ -71,10 +71,20 @@ __global__ __launch_bounds__(256) void causal_conv_kernel(const CcArgs a) {
 #pragma unroll
         for (int r = 0; r < K - 1; ++r) *(VT*)(tail + (int64_t)r * a.channels) = last[r];
     }
+    // (four rows are worked on while the next four are on their way)
+    VT ahead[U];
+    auto fetch = [&](int t) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            ahead[u] = zero;
+            if (t + u < t1) ahead[u] = *(const VT*)(x + (int64_t)(t + u) * a.x_stride);
+        }
+    };
+    fetch(t0);
     for (int t = t0; t < t1; t += U) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            row[K - 1 + u] = t + u < t1 ? *(const VT*)(x + (int64_t)(t + u) * a.x_stride) : zero;
+        for (int u = 0; u < U; ++u) row[K - 1 + u] = ahead[u];
+        if (t + U < t1) fetch(t + U);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             VT out;

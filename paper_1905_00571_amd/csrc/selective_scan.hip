@@ -60,6 +60,35 @@ __device__ __forceinline__ float ss_sum(float v) {
     return v;
 }
 
+// NS consecutive floats of a lane, `left` of which exist; 16 bytes at a time where all do (4-byte alignment is enough).
+template <int NS>
+__device__ __forceinline__ void ss_load(const float* p, int left, float (&v)[NS]) {
+    typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
+    if (left >= NS) {
+#pragma unroll
+        for (int k = 0; k < NS; k += 4) {
+            const F4 q = *(const F4*)(p + k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[k + e] = q[e];
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < NS; ++k) v[k] = k < left ? p[k] : 0.0f;
+    }
+}
+template <int NS>
+__device__ __forceinline__ void ss_store(float* p, int left, const float (&v)[NS]) {
+    typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
+    if (left >= NS) {
+#pragma unroll
+        for (int k = 0; k < NS; k += 4) *(F4*)(p + k) = (F4){v[k], v[k + 1], v[k + 2], v[k + 3]};
+    } else {
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+            if (k < left) p[k] = v[k];
+    }
+}
+
 enum ScanPass {
     SCAN_WHOLE,     // one pass over whole sequences
     SCAN_ENDS,      // of every piece: the state it ends with when it starts from zero
@@ -67,14 +96,16 @@ enum ScanPass {
 };
 
 // L lanes hold a channel's states, NS each.  The inputs of kScanTile tokens are fetched while the tile before them is
-// worked on; b and c, which all channels of a group share, go through LDS as fp32.  FULL: dstate = NS * L; else the
+// worked on; b and c, which all channels of a group share, go through LDS.  FULL: dstate = NS * L; else the
 // states behind the last one stay zero whatever x and dt are.
 template <typename T, int NS, int L, int PASS, bool FULL>
 __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
     constexpr int CH = 256 / L, N = NS * L, TT = kScanTile;
-    constexpr int ROW = PASS == SCAN_ENDS ? N : 2 * N;          // floats of a token in LDS
+    constexpr int ROW = PASS == SCAN_ENDS ? N : 2 * N;          // elements of a token in LDS
     constexpr int PER = (TT * ROW + 255) / 256;                 // of them fetched by a thread
-    __shared__ __attribute__((aligned(16))) float bc[2][TT * ROW];
+    constexpr int V = 16 / (int)sizeof(T);
+    typedef T VT __attribute__((ext_vector_type(V)));
+    __shared__ __attribute__((aligned(16))) T bc[2][TT * ROW];
     const int tid = (int)threadIdx.x, sub = tid % L;
     const int grp = (int)blockIdx.y / a.blocks_per_group;
     const int in_group = ((int)blockIdx.y - grp * a.blocks_per_group) * CH + tid / L;
@@ -97,44 +128,62 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
         t1 = (int)min((int64_t)hi, first + a.chunk);
     }
     if (t0 >= t1) return;
-    float h[NS], al[NS];
-    float* kept = nullptr;
-    if (PASS == SCAN_WHOLE) kept = a.state ? a.state + ((int64_t)s * a.channels + ch) * a.dstate : nullptr;
-    else kept = a.part + (slot * a.channels + ch) * a.dstate;
-#pragma unroll
-    for (int k = 0; k < NS; ++k) {
-        const int n = sub * NS + k;
-        al[k] = n < a.dstate ? a.a[(int64_t)ch * a.dstate + n] * 1.44269502f : 0.0f;
-        h[k] = PASS != SCAN_ENDS && kept && n < a.dstate ? kept[n] : 0.0f;
-    }
-    const float bias = a.dt_bias ? a.dt_bias[ch] : 0.0f;
-    const float dv = a.d ? a.d[ch] : 0.0f;
-    const T* xp = (const T*)a.x + ch;
-    const T* dp = (const T*)a.dt + ch;
-    const T* zp = (const T*)a.z + ch;
-    T* yp = (T*)a.y + ch;
+    // (rows are uniform, channels are the lanes': a scalar base and a 32-bit offset address a load)
+    const uint32_t lane_at = (uint32_t)ch * (uint32_t)sizeof(T);
+    auto elem = [&](const void* base, int64_t stride, int at) -> T { return *(const T*)((const char*)base + at * stride * (int64_t)sizeof(T) + lane_at); };
     const T* bp = (const T*)a.b + (int64_t)grp * a.dstate;
     const T* cp = (const T*)a.c + (int64_t)grp * a.dstate;
     T nx[TT], nd[TT], nz[TT];
-    float nb[PER];
+    T nb[PER];
     auto fetch = [&](int t) {
+        if (t + TT <= t1) {
+            const char *x = (const char*)a.x + t * a.x_stride * (int64_t)sizeof(T), *d = (const char*)a.dt + t * a.dt_stride * (int64_t)sizeof(T);
+            const char* z = a.z ? (const char*)a.z + t * a.z_stride * (int64_t)sizeof(T) : nullptr;
 #pragma unroll
-        for (int u = 0; u < TT; ++u) {
-            const int at = min(t + u, t1 - 1);
-            nx[u] = xp[(int64_t)at * a.x_stride];
-            nd[u] = dp[(int64_t)at * a.dt_stride];
-            if (PASS != SCAN_ENDS) nz[u] = a.z ? zp[(int64_t)at * a.z_stride] : (T)0.0f;
+            for (int u = 0; u < TT; ++u) {
+                nx[u] = *(const T*)(x + lane_at);
+                nd[u] = *(const T*)(d + lane_at);
+                x += a.x_stride * (int64_t)sizeof(T);
+                d += a.dt_stride * (int64_t)sizeof(T);
+                if (PASS != SCAN_ENDS && z) {
+                    nz[u] = *(const T*)(z + lane_at);
+                    z += a.z_stride * (int64_t)sizeof(T);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < TT; ++u) {
+                const int at = min(t + u, t1 - 1);
+                nx[u] = elem(a.x, a.x_stride, at);
+                nd[u] = elem(a.dt, a.dt_stride, at);
+                if (PASS != SCAN_ENDS && a.z) nz[u] = elem(a.z, a.z_stride, at);
+            }
         }
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             const int i = k * 256 + tid, u = i / ROW, r = i % ROW, n = r < N ? r : r - N, at = t + u;
-            float v = 0.0f;
+            T v = (T)0.0f;
             if (i < TT * ROW && at < t1 && n < a.dstate)
-                v = r < N ? (float)bp[(int64_t)at * a.b_stride + n] : (float)cp[(int64_t)at * a.c_stride + n];
+                v = r < N ? bp[(int64_t)at * a.b_stride + n] : cp[(int64_t)at * a.c_stride + n];
             nb[k] = v;
         }
     };
     fetch(t0);
+    float h[NS], al[NS];
+    const int n_left = a.dstate - sub * NS;
+    float* kept = nullptr;
+    if (PASS == SCAN_WHOLE) kept = a.state ? a.state + ((int64_t)s * a.channels + ch) * a.dstate + sub * NS : nullptr;
+    else kept = a.part + (slot * a.channels + ch) * a.dstate + sub * NS;
+    ss_load<NS>(a.a + (int64_t)ch * a.dstate + sub * NS, FULL ? NS : n_left, al);
+    if (PASS != SCAN_ENDS && kept) ss_load<NS>(kept, FULL ? NS : n_left, h);
+    else {
+#pragma unroll
+        for (int k = 0; k < NS; ++k) h[k] = 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < NS; ++k) al[k] *= 1.44269502f;
+    const float bias = a.dt_bias ? a.dt_bias[ch] : 0.0f;
+    const float dv = a.d ? a.d[ch] : 0.0f;
     float span = 0.0f;
     int buf = 0;
     for (int t = t0; t < t1; t += TT, buf ^= 1) {
@@ -143,51 +192,67 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
         for (int u = 0; u < TT; ++u) {
             x[u] = (float)nx[u];
             dt[u] = (float)nd[u];
-            z[u] = PASS != SCAN_ENDS ? (float)nz[u] : 0.0f;
+            z[u] = PASS != SCAN_ENDS && a.z ? (float)nz[u] : 0.0f;
         }
 #pragma unroll
         for (int k = 0; k < PER; ++k)
             if (k * 256 + tid < TT * ROW) bc[buf][k * 256 + tid] = nb[k];
         __syncthreads();     // (the other buffer is written next, after the next barrier's readers of this one)
         if (t + TT < t1) fetch(t + TT);
-        const int left = min(TT, t1 - t);
+        const int left = t1 - t;
         float steps = 0.0f;          // (summed by tiles: 8 + chunk / 8 roundings at most, not chunk)
 #pragma unroll
         for (int u = 0; u < TT; ++u) {
-            if (u < left) {
-                float step = dt[u] + bias;
-                if (a.softplus) step = ss_softplus(step);
-                const float in = step * x[u];
-                const float* row = bc[buf] + u * ROW + sub * NS;
-                float y = 0.0f;
-#pragma unroll
-                for (int k = 0; k < NS; ++k) {
-                    h[k] = fmaf(ss_exp2(step * al[k]), h[k], in * row[k]);
-                    if (!FULL) h[k] = sub * NS + k < a.dstate ? h[k] : 0.0f;
-                    if (PASS != SCAN_ENDS) y = fmaf(row[N + k], h[k], y);
-                }
-                if (PASS == SCAN_ENDS) {
-                    steps += step;
-                } else {
-                    y = ss_sum<L>(y);
-                    y = fmaf(dv, x[u], y);
-                    if (a.z) y *= ss_silu(z[u]);
-                    if (sub == 0 && real) yp[(int64_t)(t + u) * a.y_stride] = (T)y;
-                }
-            }
+            dt[u] += bias;
+            if (a.softplus) dt[u] = ss_softplus(dt[u]);
+            if (PASS == SCAN_ENDS) steps += u < left ? dt[u] : 0.0f;
+            else if (a.z) z[u] = ss_silu(z[u]);
         }
         span += steps;
+        char* yt = (char*)a.y + t * a.y_stride * (int64_t)sizeof(T);
+        // one token: three full-rate operations a state beside the exponential and the product under it
+        auto token = [&](int u) {
+            const float step = dt[u], in = step * x[u];
+            const T* row = bc[buf] + u * ROW + sub * NS;
+            float y = 0.0f;
+#pragma unroll
+            for (int k0 = 0; k0 < NS; k0 += V) {
+                const VT bv = *(const VT*)(row + k0);
+                VT cv = bv;
+                if (PASS != SCAN_ENDS) cv = *(const VT*)(row + N + k0);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const int k = k0 + e;
+                    h[k] = fmaf((float)bv[e], in, ss_exp2(step * al[k]) * h[k]);
+                    if (!FULL) h[k] = sub * NS + k < a.dstate ? h[k] : 0.0f;
+                    if (PASS != SCAN_ENDS) y = fmaf((float)cv[e], h[k], y);
+                }
+            }
+            if (PASS != SCAN_ENDS) {
+                y = ss_sum<L>(y);
+                y = fmaf(dv, x[u], y);
+                if (a.z) y *= z[u];
+                if (sub == 0 && real) *(T*)(yt + lane_at) = (T)y;
+                yt += a.y_stride * (int64_t)sizeof(T);
+            }
+        };
+        if (left >= TT) {
+#pragma unroll
+            for (int u = 0; u < TT; ++u) token(u);
+        } else {
+#pragma unroll
+            for (int u = 0; u < TT; ++u)
+                if (u < left) token(u);
+        }
     }
     if (real && kept && PASS != SCAN_PIECES) {
-#pragma unroll
-        for (int k = 0; k < NS; ++k)
-            if (sub * NS + k < a.dstate) kept[sub * NS + k] = h[k];
+        ss_store<NS>(kept, FULL ? NS : n_left, h);
         if (PASS == SCAN_ENDS && sub == 0) a.span[slot * a.channels + ch] = span;
     }
 }
 
 // Joins the pieces of each sequence: h = exp(a * span) * h + end, one thread per (sequence, channel, state).  What a piece
-// ended with is replaced by what it starts from; four pieces are fetched at a time.
+// ended with is replaced by what it starts from; sixteen pieces are fetched at a time.
 __global__ __launch_bounds__(256) void scan_join_kernel(const SsArgs a) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per_seq = (int64_t)a.channels * a.dstate;
     if (i >= per_seq) return;
@@ -201,7 +266,7 @@ __global__ __launch_bounds__(256) void scan_join_kernel(const SsArgs a) {
     const float al = a.a[i] * 1.44269502f;
     float* kept = a.state ? a.state + (int64_t)s * per_seq + i : nullptr;
     float h = kept ? *kept : 0.0f;
-    constexpr int U = 4;
+    constexpr int U = 16;
     for (int p = 0; p < pieces; p += U) {
         float end[U], span[U];
 #pragma unroll
@@ -224,42 +289,33 @@ __global__ __launch_bounds__(256) void scan_join_kernel(const SsArgs a) {
     if (kept) *kept = h;
 }
 
-// Few tokens a sequence: L lanes hold a channel's states, four each, read and written as 16 bytes where they are aligned;
-// b and c come straight from memory.
-template <typename T, int L, bool VEC>
+// Few tokens a sequence: L lanes hold a channel's states, four each, so that a wave reads and writes them in whole
+// kilobytes; b and c come straight from memory.
+template <typename T, int L>
 __global__ __launch_bounds__(256) void scan_few_kernel(const SsArgs a) {
-    const int64_t i = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-    const int sub = (int)threadIdx.x % L, n0 = sub * 4;
-    const bool real = i < (int64_t)a.channels;
-    const int ch = real ? (int)i : a.channels - 1;
+    typedef T V4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    const int i = (int)blockIdx.x * (256 / L) + (int)threadIdx.x / L;
+    const int n0 = ((int)threadIdx.x % L) * 4;
+    const bool real = i < a.channels;
+    const int ch = real ? i : a.channels - 1;
     const int s = (int)blockIdx.y;
     int lo, hi;
     seq_range(a.q, s, &lo, &hi);
     if (lo >= hi) return;
-    const int grp = ch / a.per;
+    const int grp = a.groups == 1 ? 0 : ch / a.per;
+    const int left = min(4, a.dstate - n0);       // states of the lane that exist, none or fewer for the last lanes
     float h[4], al[4];
     float* kept = a.state ? a.state + ((int64_t)s * a.channels + ch) * a.dstate + n0 : nullptr;
-    const float* ap = a.a + (int64_t)ch * a.dstate + n0;
-    typedef float F4 __attribute__((ext_vector_type(4)));
-    const bool whole = VEC && n0 < a.dstate;
-    if (whole) {
-        const F4 av = *(const F4*)ap;
-        F4 hv = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (kept) hv = *(const F4*)kept;
+    if (kept) ss_load<4>(kept, left, h);
+    else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) { al[k] = av[k]; h[k] = hv[k]; }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const bool in = n0 + k < a.dstate;
-            al[k] = in ? ap[k] : 0.0f;
-            h[k] = in && kept ? kept[k] : 0.0f;
-        }
+        for (int k = 0; k < 4; ++k) h[k] = 0.0f;
     }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) al[k] *= 1.44269502f;
+    ss_load<4>(a.a + (int64_t)ch * a.dstate + n0, left, al);
     const float bias = a.dt_bias ? a.dt_bias[ch] : 0.0f;
     const float dv = a.d ? a.d[ch] : 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) al[k] *= 1.44269502f;
     for (int t = lo; t < hi; ++t) {
         const float x = (float)((const T*)a.x)[(int64_t)t * a.x_stride + ch];
         float step = (float)((const T*)a.dt)[(int64_t)t * a.dt_stride + ch] + bias;
@@ -267,37 +323,31 @@ __global__ __launch_bounds__(256) void scan_few_kernel(const SsArgs a) {
         const T* bp = (const T*)a.b + (int64_t)t * a.b_stride + (int64_t)grp * a.dstate + n0;
         const T* cp = (const T*)a.c + (int64_t)t * a.c_stride + (int64_t)grp * a.dstate + n0;
         float bv[4], cv[4];
+        if (left == 4) {
+            const V4 b4 = *(const V4*)bp, c4 = *(const V4*)cp;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const bool in = n0 + k < a.dstate;
-            bv[k] = in ? (float)bp[k] : 0.0f;
-            cv[k] = in ? (float)cp[k] : 0.0f;
+            for (int k = 0; k < 4; ++k) { bv[k] = (float)b4[k]; cv[k] = (float)c4[k]; }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                bv[k] = k < left ? (float)bp[k] : 0.0f;
+                cv[k] = k < left ? (float)cp[k] : 0.0f;
+            }
         }
         if (a.softplus) step = ss_softplus(step);
         const float in = step * x;
         float y = 0.0f;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            h[k] = n0 + k < a.dstate ? fmaf(ss_exp2(step * al[k]), h[k], in * bv[k]) : 0.0f;
+            h[k] = k < left ? fmaf(bv[k], in, ss_exp2(step * al[k]) * h[k]) : 0.0f;
             y = fmaf(cv[k], h[k], y);
         }
         y = ss_sum<L>(y);
         y = fmaf(dv, x, y);
         if (a.z) y *= ss_silu(z);
-        if (sub == 0 && real) ((T*)a.y)[(int64_t)t * a.y_stride + ch] = (T)y;
+        if (n0 == 0 && real) ((T*)a.y)[(int64_t)t * a.y_stride + ch] = (T)y;
     }
-    if (real && kept) {
-        if (whole) {
-            F4 hv;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) hv[k] = h[k];
-            *(F4*)kept = hv;
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (n0 + k < a.dstate) kept[k] = h[k];
-        }
-    }
+    if (real && kept) ss_store<4>(kept, left, h);
 }
 
 template <typename T, int NS, int L, int PASS, bool FULL>
@@ -359,9 +409,7 @@ hipError_t launch_scan_lanes(const SsArgs& a, hipStream_t s) {
 template <typename T, int L>
 hipError_t launch_few_lanes(const SsArgs& a, hipStream_t s) {
     const dim3 grid((unsigned)((a.channels + 256 / L - 1) / (256 / L)), (unsigned)a.q.seqs);
-    const bool vec = a.dstate % 4 == 0 && (uintptr_t)a.state % 16 == 0 && (uintptr_t)a.a % 16 == 0;
-    if (vec) CADNN_LAUNCH((scan_few_kernel<T, L, true>), grid, dim3(256), 0, s, a);
-    else CADNN_LAUNCH((scan_few_kernel<T, L, false>), grid, dim3(256), 0, s, a);
+    CADNN_LAUNCH((scan_few_kernel<T, L>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
