@@ -6,6 +6,8 @@
 // element once and does K multiply-adds with it: memory bounds it, and the launch itself for single tokens.  A thread owns
 // 16 bytes of a row (its channels' taps stay in registers) and a run of tokens, over which it slides a window of rows, four
 // rows loaded at a time; K - 1 rows of a run are read twice.
+#include <type_traits>
+
 #include "q4.h"
 #include "sequence.h"
 
@@ -71,6 +73,12 @@ __global__ __launch_bounds__(256) void causal_conv_kernel(const CcArgs a) {
 #pragma unroll
         for (int r = 0; r < K - 1; ++r) *(VT*)(tail + (int64_t)r * a.channels) = last[r];
     }
+    // A tap that is exactly zero is not applied, whatever it would meet; a wave without one does not look.
+    bool zeros = false;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int k = 0; k < K; ++k) zeros |= w[v][k] == 0.0f;
     // (four rows are worked on while the next four are on their way)
     VT ahead[U];
     auto fetch = [&](int t) {
@@ -81,26 +89,29 @@ __global__ __launch_bounds__(256) void causal_conv_kernel(const CcArgs a) {
         }
     };
     fetch(t0);
-    for (int t = t0; t < t1; t += U) {
+    auto run = [&](auto skip) {
+        for (int t = t0; t < t1; t += U) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) row[K - 1 + u] = ahead[u];
-        if (t + U < t1) fetch(t + U);
+            for (int u = 0; u < U; ++u) row[K - 1 + u] = ahead[u];
+            if (t + U < t1) fetch(t + U);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            VT out;
+            for (int u = 0; u < U; ++u) {
+                VT out;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float acc = b[v];
-                // (a tap that is exactly zero is not applied, whatever it would meet)
+                for (int v = 0; v < V; ++v) {
+                    float acc = b[v];
 #pragma unroll
-                for (int k = 0; k < K; ++k) acc = w[v][k] != 0.0f ? fmaf(w[v][k], (float)row[u + k][v], acc) : acc;
-                out[v] = (T)apply_act(acc, a.act);
+                    for (int k = 0; k < K; ++k) acc = !skip.value || w[v][k] != 0.0f ? fmaf(w[v][k], (float)row[u + k][v], acc) : acc;
+                    out[v] = (T)apply_act(acc, a.act);
+                }
+                if (t + u < t1) *(VT*)(y + (int64_t)(t + u) * a.y_stride) = out;
             }
-            if (t + u < t1) *(VT*)(y + (int64_t)(t + u) * a.y_stride) = out;
-        }
 #pragma unroll
-        for (int r = 0; r < K - 1; ++r) row[r] = row[r + U];
-    }
+            for (int r = 0; r < K - 1; ++r) row[r] = row[r + U];
+        }
+    };
+    if (__any(zeros)) run(std::true_type{});
+    else run(std::false_type{});
 }
 
 template <typename T, int V, int K>

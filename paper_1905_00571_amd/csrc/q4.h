@@ -29,9 +29,19 @@ cadnn_status launch_q4_fc(const cadnn_q4_weights* w, const void* x, int64_t x_st
 // not be captured while memory is still to be allocated (NULL: none).
 cadnn_status ensure_q4_device(const cadnn_q4_weights* w, const char* who, hipStream_t capturing, bool has_stream);
 
+// v / (1 + exp(-v)), to about 6 half steps of the value: the exponent's product with log2(e) is taken in two parts, so that its
+// rounding does not grow with v.  (Below -150, where the quotient is zero, the parts could be infinite.)  A third of the
+// instructions of the library's exponential and quotient, which bounded the fp16 convolution.
+__device__ __forceinline__ float act_silu(float v) {
+    const float u = v < -150.0f ? 150.0f : -v;
+    const float hi = u * 1.44269502f, lo = fmaf(u, 1.44269502f, -hi) + u * 1.92596303e-8f;
+    const float e = __builtin_amdgcn_exp2f(hi);
+    return v * __builtin_amdgcn_rcpf(fmaf(e, fmaf(lo, 0.693147182f, 1.0f), 1.0f));
+}
+
 __device__ __forceinline__ float apply_act(float v, int act) {
     if (act == CADNN_ACT_RELU) return v > 0.0f ? v : 0.0f;
-    if (act == CADNN_ACT_SILU) return v / (1.0f + expf(-v));
+    if (act == CADNN_ACT_SILU) return act_silu(v);
     return v;
 }
 

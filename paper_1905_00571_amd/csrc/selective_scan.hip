@@ -7,6 +7,8 @@
 // Every (t, c, n) costs an exponential (a quarter of the vector rate) and four full-rate operations, about 32 cycles of a
 // SIMD per 64 of them, against 2 / N elements of traffic: from N = 16 on the vector units bound a long scan, and the
 // states' traffic a single token.
+#include <type_traits>
+
 #include "sequence.h"
 
 namespace cadnn {
@@ -251,11 +253,53 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
     }
 }
 
-// Joins the pieces of each sequence: h = exp(a * span) * h + end, one thread per (sequence, channel, state).  What a piece
-// ended with is replaced by what it starts from; sixteen pieces are fetched at a time.
+// Joins the pieces of each sequence, h = exp(a * span) * h + end; what a piece ended with is replaced by what it starts from.
+// A workgroup owns 64 (channel, state) pairs of a sequence.  Its four waves fetch S pieces each, join them from zero, learn
+// from each other what they start from, and go through them again, in registers: the chain of a long sequence costs one
+// round trip to memory for 4 * S pieces.  (One thread for a pair's whole chain took 12.5 us for 64 pieces of 32768 pairs.)
+template <int S>
+__device__ __forceinline__ float ss_join(const SsArgs& a, int64_t per_seq, int64_t i, int ch, int64_t first, int p0, int pieces, float al, float h, float (&lds)[2][4][64]) {
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+    float end[S], f[S];
+#pragma unroll
+    for (int u = 0; u < S; ++u) {
+        const int p = p0 + wave * S + u;
+        const int64_t slot = first + min(p, pieces - 1);
+        const bool there = p < pieces && slot < a.slots;
+        end[u] = there ? a.part[slot * per_seq + i] : 0.0f;
+        f[u] = there ? a.span[slot * a.channels + ch] : 0.0f;
+    }
+    float all = 1.0f, own = 0.0f;
+#pragma unroll
+    for (int u = 0; u < S; ++u) {
+        // (not below the smallest normal number: an infinite state outlives any number of steps that each shrink it a little)
+        f[u] = fmaxf(ss_exp2(al * f[u]), 0x1p-126f);
+        own = fmaf(f[u], own, end[u]);
+        all = fmaxf(all * f[u], 0x1p-126f);
+    }
+    lds[0][wave][lane] = all;
+    lds[1][wave][lane] = own;
+    __syncthreads();
+    float mine = h;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (w == wave) mine = h;
+        h = fmaf(lds[0][w][lane], h, lds[1][w][lane]);
+    }
+#pragma unroll
+    for (int u = 0; u < S; ++u) {
+        const int p = p0 + wave * S + u;
+        if (p < pieces && first + p < a.slots) a.part[(first + p) * per_seq + i] = mine;
+        mine = fmaf(f[u], mine, end[u]);
+    }
+    __syncthreads();
+    return h;
+}
+
 __global__ __launch_bounds__(256) void scan_join_kernel(const SsArgs a) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per_seq = (int64_t)a.channels * a.dstate;
-    if (i >= per_seq) return;
+    __shared__ float lds[2][4][64];
+    const int64_t per_seq = (int64_t)a.channels * a.dstate, at = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+    const int64_t i = min(at, per_seq - 1);      // (lanes behind the last pair repeat it: same reads before, same values written)
     const int s = (int)blockIdx.y;
     int lo, hi;
     seq_range(a.q, s, &lo, &hi);
@@ -266,25 +310,45 @@ __global__ __launch_bounds__(256) void scan_join_kernel(const SsArgs a) {
     const float al = a.a[i] * 1.44269502f;
     float* kept = a.state ? a.state + (int64_t)s * per_seq + i : nullptr;
     float h = kept ? *kept : 0.0f;
-    constexpr int U = 16;
+    int p = 0;
+    for (; pieces - p > 32; p += 128) h = ss_join<32>(a, per_seq, i, ch, first, p, pieces, al, h, lds);
+    for (; p < pieces; p += 32) h = ss_join<8>(a, per_seq, i, ch, first, p, pieces, al, h, lds);
+    if (kept && at < per_seq && threadIdx.x < 64) *kept = h;
+}
+
+// The same for sequences of few pieces: one thread for a pair's whole chain, four pieces fetched at a time.
+__global__ __launch_bounds__(256) void scan_join_few_kernel(const SsArgs a) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per_seq = (int64_t)a.channels * a.dstate;
+    if (i >= per_seq) return;
+    const int s = (int)blockIdx.y;
+    int lo, hi;
+    seq_range(a.q, s, &lo, &hi);
+    if (lo >= hi) return;
+    const int ch = (int)(i / a.dstate);
+    const int64_t first = seq_first_slot(a.q, s, a.chunk);
+    const int pieces = (int)min(((int64_t)hi - lo + a.chunk - 1) / a.chunk, a.slots - first);
+    const float al = a.a[i] * 1.44269502f;
+    float* kept = a.state ? a.state + (int64_t)s * per_seq + i : nullptr;
+    float h = kept ? *kept : 0.0f;
+    float* part = a.part + first * per_seq + i;
+    const float* span = a.span + first * a.channels + ch;
+    constexpr int U = 4;
     for (int p = 0; p < pieces; p += U) {
-        float end[U], span[U];
+        float end[U] = {}, f[U] = {};
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t slot = first + min(p + u, pieces - 1);
-            const bool there = slot < a.slots;
-            end[u] = there ? a.part[slot * per_seq + i] : 0.0f;
-            span[u] = there ? a.span[slot * a.channels + ch] : 0.0f;
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t slot = first + p + u;
-            if (p + u < pieces && slot < a.slots) {
-                a.part[slot * per_seq + i] = h;
-                // (not below the smallest normal number: an infinite state outlives any number of steps that each shrink it a little)
-                h = fmaf(fmaxf(ss_exp2(al * span[u]), 0x1p-126f), h, end[u]);
+        for (int u = 0; u < U; ++u)
+            if (p + u < pieces) {
+                end[u] = part[u * per_seq];
+                f[u] = span[(int64_t)u * a.channels];
             }
-        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p + u < pieces) {
+                part[u * per_seq] = h;
+                h = fmaf(fmaxf(ss_exp2(al * f[u]), 0x1p-126f), h, end[u]);
+            }
+        part += U * per_seq;
+        span += (int64_t)U * a.channels;
     }
     if (kept) *kept = h;
 }
@@ -383,7 +447,7 @@ ScanPlan plan_scan(const cadnn_scan_args& g) {
     const int64_t waves = (int64_t)g.seqs * g.groups * p.blocks_per_group * 4;
     if (waves >= 2048 || average < 128) return p;
     p.chunk = 512;
-    while (p.chunk > 64 && seq_slots(g.tokens, g.seqs, g.seq_start != nullptr, p.chunk) * g.groups * p.blocks_per_group * 4 < 2048) p.chunk /= 2;
+    while (p.chunk > 32 && seq_slots(g.tokens, g.seqs, g.seq_start != nullptr, p.chunk) * g.groups * p.blocks_per_group * 4 < 2048) p.chunk /= 2;
     p.slots = seq_slots(g.tokens, g.seqs, g.seq_start != nullptr, p.chunk);
     p.part_bytes = (size_t)p.slots * g.channels * g.dstate * 4;
     p.bytes = p.part_bytes + (size_t)p.slots * g.channels * 4;
@@ -396,7 +460,8 @@ hipError_t launch_scan_passes(const SsArgs& a, hipStream_t s) {
     hipError_t e = launch_scan_pass<T, NS, L, SCAN_ENDS, FULL>(a, s);
     if (e != hipSuccess) return e;
     const int64_t per_seq = (int64_t)a.channels * a.dstate;
-    CADNN_LAUNCH(scan_join_kernel, dim3((unsigned)((per_seq + 255) / 256), (unsigned)a.q.seqs), dim3(256), 0, s, a);
+    if (a.q.tokens / a.q.seqs > 16 * a.chunk) CADNN_LAUNCH(scan_join_kernel, dim3((unsigned)((per_seq + 63) / 64), (unsigned)a.q.seqs), dim3(256), 0, s, a);
+    else CADNN_LAUNCH(scan_join_few_kernel, dim3((unsigned)((per_seq + 255) / 256), (unsigned)a.q.seqs), dim3(256), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     return launch_scan_pass<T, NS, L, SCAN_PIECES, FULL>(a, s);
 }
