@@ -417,78 +417,90 @@ def cadnn_q4_prepare(w: Q4Weights) -> None:
     _check(lib().cadnn_q4_prepare(w.handle))
 
 
-def _rows(t, name: str, dtype, shape, device=None):
-    """A tensor whose rows are contiguous (a slice of a wider one may be): its distance between rows."""
-    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} is not a CUDA tensor {list(shape)} of {dtype}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} is on another device than the other tensors")
+def _rows(t, name: str, dtype, dev: int, shape) -> int:
+    """Checks a tensor whose rows are contiguous (a slice of a wider one may be) and lie on CUDA device
+    `dev`; returns the elements from one row to the next.  (Single tokens are served by calls of a
+    few microseconds: these checks and what follows them are kept to what each call needs.)"""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape:
+        raise ValueError(f"{name} is not a tensor {list(shape)} of {dtype} on cuda:{dev}")
     if t.is_contiguous():
-        return t.numel() // t.shape[0] if t.shape[0] else 1
-    inner = 1
-    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if size != 1 and stride != inner:
+        return shape[1] if len(shape) == 2 else shape[1] * shape[2]
+    strides, inner = t.stride(), 1
+    for k in range(len(shape) - 1, 0, -1):
+        if shape[k] != 1 and strides[k] != inner:
             raise ValueError(f"the rows of {name} are not contiguous")
-        inner *= size
-    return max(int(t.stride(0)), inner) if t.shape[0] == 1 else int(t.stride(0))
+        inner *= shape[k]
+    return strides[0] if shape[0] > 1 else max(strides[0], inner)
 
 
-def _whole(t, name: str, dtype, shape, device) -> None:
-    if not t.is_cuda or t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{name} is not a contiguous tensor {list(shape)} of {dtype} on {device}")
+def _whole(t, name: str, dtype, dev: int, shape) -> int:
+    """Checks a contiguous tensor on CUDA device `dev`; returns its address."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} is not a contiguous tensor {list(shape)} of {dtype} on cuda:{dev}")
+    return t.data_ptr()
 
 
-class _On:
-    """Makes the tensors' device and the call's stream (`stream`, or that device's current one) the
-    current ones: what is allocated inside belongs to that stream.  `mark` keeps the memory of
-    tensors of another stream from being handed out again before the call is through."""
-    __slots__ = ("_device", "_stream", "_context", "_foreign", "ptr")
+class _Elsewhere:
+    """For a call on a given stream, or on tensors of a device that is not the current one: makes that
+    device and stream the current ones, so that what is allocated inside belongs to the stream, and
+    keeps the memory of the caller's tensors from being handed out again before the call is through."""
 
-    def __init__(self, device, stream):
-        self._device, self._stream, self._context, self._foreign = device, stream, None, False
-
-    def __enter__(self):
+    def __init__(self, dev: int, stream, tensors):
         import torch
-        if self._stream is None and self._device.index == torch.cuda.current_device():
-            self.ptr = int(torch.cuda.current_stream().cuda_stream)
-            return self
-        if self._stream is not None and self._stream.device != self._device:
+        if stream is not None and stream.device.index != dev:
             raise ValueError("the stream belongs to another device than the tensors")
-        current = torch.cuda.current_stream(self._device)
-        s = current if self._stream is None else self._stream
-        self._foreign = s != current
-        self._context = torch.cuda.stream(s)
-        self._context.__enter__()
-        self.ptr = int(s.cuda_stream)
-        return self
-
-    def mark(self, *tensors) -> None:
-        if self._foreign:
+        current = torch.cuda.current_stream(dev)
+        self.stream = current if stream is None else stream
+        if self.stream != current:
             for t in tensors:
                 if t is not None:
-                    t.record_stream(self._stream)
+                    t.record_stream(self.stream)
+        self.context = torch.cuda.stream(self.stream)
+
+    def __enter__(self):
+        self.context.__enter__()
+        return int(self.stream.cuda_stream)
 
     def __exit__(self, *exc):
-        if self._context is not None:
-            self._context.__exit__(*exc)
+        return self.context.__exit__(*exc)
+
+
+def _cuda_index(x, name: str = "x") -> int:
+    dev = x.get_device()
+    if dev < 0 or not x.is_cuda:
+        raise ValueError(f"{name} is not on a GPU")
+    return dev
+
+
+def _here(dev: int, stream) -> bool:
+    import torch
+    return stream is None and dev == torch.cuda.current_device()
+
+
+def _stream_of(dev: int) -> int:
+    """The current stream of device `dev` (which is the current one) as a hipStream_t."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)       # (2.8 us less than building a torch.cuda.Stream)
+    return _stream_ptr() if raw is None else raw(dev)
 
 
 def cadnn_q4_fc(w: Q4Weights, x, bias=None, act: int = ACT_NONE, out=None, stream=None):
     """x: CUDA tensor [n][cin] with contiguous rows (a slice of a wider tensor may be passed); returns (or fills) [n][cout]."""
-    import torch
-    dtype = _torch_dtype(w.dtype)
-    if x.dim() != 2 or x.shape[1] != w.cin:
+    shape = x.shape
+    if len(shape) != 2 or shape[1] != w.cin:
         raise ValueError("feature mismatch")
-    n = x.shape[0]
-    x_stride = _rows(x, "x", dtype, (n, w.cin))
-    if bias is not None:
-        _whole(bias, "bias", torch.float32, (w.cout,), x.device)
-    y_stride = w.cout if out is None else _rows(out, "out", dtype, (n, w.cout), x.device)
-    with _On(x.device, stream) as on:
-        on.mark(x, bias, out)
-        if out is None:
-            out = torch.empty((n, w.cout), dtype=dtype, device=x.device)
-        _check(lib().cadnn_q4_fc(w.handle, _dptr(x), x_stride, _dptr(out), y_stride, n, _dptr(bias), act, on.ptr))
+    n, cout, dev = shape[0], w.cout, _cuda_index(x)
+    if not _here(dev, stream):
+        with _Elsewhere(dev, stream, (x, bias, out)):
+            return cadnn_q4_fc(w, x, bias, act, out)
+    dtype = _torch_dtype(w.dtype)
+    x_stride = _rows(x, "x", dtype, dev, (n, w.cin))
+    if out is None:
+        out, y_stride = x.new_empty((n, cout)), cout
+    else:
+        y_stride = _rows(out, "out", dtype, dev, (n, cout))
+    _check(lib().cadnn_q4_fc(w.handle, x.data_ptr(), x_stride, out.data_ptr(), y_stride, n,
+                             None if bias is None else _whole(bias, "bias", _f32(), dev, (cout,)), act, _stream_of(dev)))
     return out
 
 
@@ -496,67 +508,61 @@ def cadnn_causal_conv1d(w: Weights, x, state=None, seq_start=None, seqs: int = 1
                         out=None, stream=None):
     """w packed from [channels][1][1][taps]; x: CUDA tensor [tokens][channels] with contiguous rows; state: [seqs][taps - 1][channels],
     replaced; seq_start: int32 [seqs + 1] on the device (None: sequences of one length)."""
-    import torch
-    dtype = _torch_dtype(w.dtype)
-    if x.dim() != 2 or x.shape[1] != w.cout:
+    shape = x.shape
+    channels = w.cout
+    if len(shape) != 2 or shape[1] != channels:
         raise ValueError("channel mismatch")
-    tokens = x.shape[0]
-    x_stride = _rows(x, "x", dtype, (tokens, w.cout))
-    if state is not None:
-        _whole(state, "state", dtype, (seqs, w.kw - 1, w.cout), x.device)
-    if seq_start is not None:
-        _whole(seq_start, "seq_start", torch.int32, (seqs + 1,), x.device)
-    if bias is not None:
-        _whole(bias, "bias", torch.float32, (w.cout,), x.device)
-    y_stride = w.cout if out is None else _rows(out, "out", dtype, (tokens, w.cout), x.device)
-    with _On(x.device, stream) as on:
-        on.mark(x, state, seq_start, bias, out)
-        if out is None:
-            out = torch.empty((tokens, w.cout), dtype=dtype, device=x.device)
-        _check(lib().cadnn_causal_conv1d(w.handle, _dptr(x), x_stride, _dptr(out), y_stride, tokens, seqs, _dptr(seq_start),
-                                         _dptr(state), _dptr(bias), act, on.ptr))
+    tokens, dev = shape[0], _cuda_index(x)
+    if not _here(dev, stream):
+        with _Elsewhere(dev, stream, (x, state, seq_start, bias, out)):
+            return cadnn_causal_conv1d(w, x, state, seq_start, seqs, bias, act, out)
+    dtype = _torch_dtype(w.dtype)
+    x_stride = _rows(x, "x", dtype, dev, (tokens, channels))
+    if out is None:
+        out, y_stride = x.new_empty((tokens, channels)), channels
+    else:
+        y_stride = _rows(out, "out", dtype, dev, (tokens, channels))
+    _check(lib().cadnn_causal_conv1d(
+        w.handle, x.data_ptr(), x_stride, out.data_ptr(), y_stride, tokens, seqs,
+        None if seq_start is None else _whole(seq_start, "seq_start", _i32(), dev, (seqs + 1,)),
+        None if state is None else _whole(state, "state", dtype, dev, (seqs, w.kw - 1, channels)),
+        None if bias is None else _whole(bias, "bias", _f32(), dev, (channels,)), act, _stream_of(dev)))
     return out
 
 
-def _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, out) -> ScanArgs:
+def _f32():
     import torch
-    if x.dim() != 2 or x.dtype not in (torch.float32, torch.float16):
+    return torch.float32
+
+
+def _i32():
+    import torch
+    return torch.int32
+
+
+def _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, out) -> ScanArgs:
+    f32, dtype, shape = _f32(), x.dtype, x.shape
+    if len(shape) != 2 or (dtype is not f32 and dtype is not _torch_dtype(F16)):
         raise ValueError("x is not a float32 or float16 tensor [tokens][channels]")
-    tokens, channels = x.shape
+    tokens, channels = shape
+    wide, dev = (tokens, channels), _cuda_index(x)
     if a.dim() != 2 or a.shape[0] != channels:
         raise ValueError("a is not [channels][dstate]")
     dstate = a.shape[1]
-    if b.dim() == 2:
-        b = b.unsqueeze(1)
-    if c.dim() == 2:
-        c = c.unsqueeze(1)
-    if b.dim() != 3:
-        raise ValueError("b is not [tokens][groups][dstate]")
-    groups = b.shape[1]
-    g = ScanArgs()
-    g.dtype = F16 if x.dtype == torch.float16 else F32
-    g.tokens, g.seqs, g.channels, g.dstate, g.groups, g.softplus = tokens, seqs, channels, dstate, groups, int(bool(softplus))
-    wide, narrow = (tokens, channels), (tokens, groups, dstate)
-    g.x_stride = _rows(x, "x", x.dtype, wide)
-    g.dt_stride = _rows(dt, "dt", x.dtype, wide, x.device)
-    g.b_stride = _rows(b, "b", x.dtype, narrow, x.device)
-    g.c_stride = _rows(c, "c", x.dtype, narrow, x.device)
-    _whole(a, "a", torch.float32, (channels, dstate), x.device)
-    for name, v in (("d", d), ("dt_bias", dt_bias)):
-        if v is not None:
-            _whole(v, name, torch.float32, (channels,), x.device)
-    if z is not None:
-        g.z_stride = _rows(z, "z", x.dtype, wide, x.device)
-    if state is not None:
-        _whole(state, "state", torch.float32, (seqs, channels, dstate), x.device)
-    if seq_start is not None:
-        _whole(seq_start, "seq_start", torch.int32, (seqs + 1,), x.device)
-    if out is not None:
-        g.y_stride = _rows(out, "out", x.dtype, wide, x.device)
-        g.y = _dptr(out)
-    g.x, g.dt, g.a, g.b, g.c, g.d, g.z = (_dptr(v) for v in (x, dt, a, b, c, d, z))
-    g.dt_bias, g.state, g.seq_start = _dptr(dt_bias), _dptr(state), _dptr(seq_start)
-    return g
+    groups = 1 if b.dim() == 2 else b.shape[1]
+    flat, grouped = (tokens, dstate), (tokens, groups, dstate)
+    return ScanArgs(
+        F32 if dtype is f32 else F16, tokens, seqs, channels, dstate, groups, 1 if softplus else 0,
+        None if seq_start is None else _whole(seq_start, "seq_start", _i32(), dev, (seqs + 1,)),
+        x.data_ptr(), dt.data_ptr(), b.data_ptr(), c.data_ptr(), None if z is None else z.data_ptr(),
+        None if out is None else out.data_ptr(),
+        _rows(x, "x", dtype, dev, wide), _rows(dt, "dt", dtype, dev, wide),
+        _rows(b, "b", dtype, dev, flat if b.dim() == 2 else grouped),
+        _rows(c, "c", dtype, dev, flat if c.dim() == 2 and groups == 1 else grouped),
+        0 if z is None else _rows(z, "z", dtype, dev, wide), 0 if out is None else _rows(out, "out", dtype, dev, wide),
+        _whole(a, "a", f32, dev, (channels, dstate)), None if d is None else _whole(d, "d", f32, dev, (channels,)),
+        None if dt_bias is None else _whole(dt_bias, "dt_bias", f32, dev, (channels,)),
+        None if state is None else _whole(state, "state", f32, dev, (seqs, channels, dstate)))
 
 
 def cadnn_selective_scan_workspace_bytes(x, dt, a, b, c, d=None, z=None, dt_bias=None, softplus: bool = False, state=None,
@@ -573,25 +579,26 @@ def cadnn_selective_scan(x, dt, a, b, c, d=None, z=None, dt_bias=None, softplus:
     """x, dt, z: CUDA tensors [tokens][channels]; b, c: [tokens][groups][dstate] or [tokens][dstate]; a: [channels][dstate]; state:
     [seqs][channels][dstate], replaced.  workspace: a uint8 tensor (None: one is taken from torch's allocator for the call; an empty one:
     no workspace)."""
-    import torch
+    dev = _cuda_index(x)
+    if not _here(dev, stream):
+        with _Elsewhere(dev, stream, (x, dt, a, b, c, d, z, dt_bias, state, seq_start, out, workspace)):
+            return cadnn_selective_scan(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, out, workspace)
+    if out is None:
+        out = x.new_empty(x.shape)
     g = _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, out)
-    if workspace is not None and (not workspace.is_cuda or workspace.device != x.device or workspace.dtype != torch.uint8 or not workspace.is_contiguous()):
-        raise ValueError(f"workspace is not a contiguous uint8 tensor on {x.device}")
-    with _On(x.device, stream) as on:
-        on.mark(x, dt, a, b, c, d, z, dt_bias, state, seq_start, out, workspace)
-        if out is None:
-            out = torch.empty(tuple(x.shape), dtype=x.dtype, device=x.device)
-            g.y, g.y_stride = _dptr(out), x.shape[1]
-        size = 0
-        if workspace is None:
-            nbytes = ctypes.c_size_t()
-            _check(lib().cadnn_selective_scan_workspace_bytes(ctypes.byref(g), ctypes.byref(nbytes)))
-            size = nbytes.value
-            if size:
-                workspace = torch.empty(size, dtype=torch.uint8, device=x.device)
-        else:
-            size = workspace.numel()
-        _check(lib().cadnn_selective_scan(ctypes.byref(g), _dptr(workspace) if size else None, size, on.ptr))
+    L, ref = lib(), ctypes.byref(g)
+    if workspace is None:
+        nbytes = ctypes.c_size_t()
+        _check(L.cadnn_selective_scan_workspace_bytes(ref, ctypes.byref(nbytes)))
+        size = nbytes.value
+        if size:
+            import torch
+            workspace = torch.empty(size, dtype=torch.uint8, device=x.device)
+    else:
+        import torch
+        size = workspace.numel()
+        _whole(workspace, "workspace", torch.uint8, dev, (size,))
+    _check(L.cadnn_selective_scan(ref, workspace.data_ptr() if size else None, size, _stream_of(dev)))
     return out
 
 
