@@ -216,15 +216,17 @@ __global__ __launch_bounds__(512) void q4_few_kernel(const Q4Args a) {
 // wave) into LDS, each element read, and cut apart, once, while the matrix instructions work on the chunk before, and a wave's
 // codes and scales are fetched D chunks ahead.  us at 8192 -> 8192, groups of 128, one token: fp16 10.6, fp32 12.3, where the kernel above
 // takes 14.2 and 19.6; the 35 MB are 6.4 us at the rate of a large copy.
-template <typename T, int GP, int RT, int HELD>
-__global__ __launch_bounds__(512) void q4_columns_kernel(const Q4Args a) {
+// (Two workgroups to a compute unit, which takes 128 registers: with one, the 257 tiles of 4099 filters took twice the time of 256.)
+template <typename T, int GP, int HELD>
+__global__ __launch_bounds__(512, sizeof(T) == 4 && GP == 4 && HELD > 1 ? 2 : 4) void q4_columns_kernel(const Q4Args a) {
     typedef Q4Frag<T> F;
     constexpr int P = F::kParts;
-    constexpr int D = RT * GP * (int)sizeof(T) >= 16 ? 2 : 4;
+    constexpr int D = GP == 4 ? 2 : 4;
+    typedef T S4 __attribute__((ext_vector_type(4)));
     extern __shared__ __attribute__((aligned(16))) char q4_smem[];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = (int)blockDim.x >> 6;
     const int j = lane & 15, g = lane >> 4;
-    const int tile0 = (int)blockIdx.x * RT, tiles = (a.cout + 15) / 16;
+    const int tile = (int)blockIdx.x;
     const uint32_t buf_bytes = (uint32_t)waves * 4096u;        // [block][16 columns][128 inputs], pieces of 16 bytes placed as below
     auto at = [&](uint32_t buf, int block, int col, int piece) { return q4_smem + buf * buf_bytes + block * 4096 + col * 256 + ((piece ^ col) << 4); };
     for (uint32_t i = (uint32_t)tid * 16u; i < 2 * buf_bytes; i += blockDim.x * 16u) *(q4_u4*)(q4_smem + i) = (q4_u4){0u, 0u, 0u, 0u};
@@ -252,22 +254,19 @@ __global__ __launch_bounds__(512) void q4_columns_kernel(const Q4Args a) {
             }
         }
     };
-    q4_u4 w[D][RT];
-    q4_f4 sc[D][RT][GP], acc[RT];
+    q4_u4 w[D];
+    S4 sc[D][GP];
+    q4_f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t* const code_at = a.codes + (int64_t)tile * a.blocks * 256 + lane * 4;
+    const T* const scale_at = (const T*)a.scales + (int64_t)tile * a.blocks * (GP * 16) + 4 * g;
     auto codes = [&](int slot, int chunk) {
         const int b = min(chunk * waves + wave, a.blocks - 1);      // (behind the last block the activations are zero)
+        w[slot] = *(const q4_u4*)(code_at + (int64_t)b * 256);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            const int64_t block = (int64_t)min(tile0 + r, tiles - 1) * a.blocks + b;
-            w[slot][r] = *(const q4_u4*)(a.codes + block * 256 + lane * 4);
-#pragma unroll
-            for (int p = 0; p < GP; ++p) sc[slot][r][p] = q4_scales((const T*)a.scales + (block * GP + p) * 16 + 4 * g);
-        }
+        for (int p = 0; p < GP; ++p) sc[slot][p] = *(const S4*)(scale_at + ((int64_t)b * GP + p) * 16);
     };
 #pragma unroll
     for (int d = 0; d < D; ++d) codes(d, d);
-#pragma unroll
-    for (int r = 0; r < RT; ++r) acc[r] = (q4_f4){0.0f, 0.0f, 0.0f, 0.0f};
     fetch(0);
     put(0);
     __syncthreads();
@@ -279,17 +278,14 @@ __global__ __launch_bounds__(512) void q4_columns_kernel(const Q4Args a) {
             const int c = c0 + d;
             if (c < chunks) {
                 if (c + 1 < chunks) fetch(c + 1);
-                q4_f4 sum[RT];
+                q4_f4 sum;
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
                     const typename F::V xf = *(const typename F::V*)at(buf, wave, j, s * 4 + g);
+                    sum = F::mul(F::codes(w[d][s]), xf, s % (4 / GP) == 0 ? (q4_f4){0.0f, 0.0f, 0.0f, 0.0f} : sum);
+                    if ((s + 1) % (4 / GP) == 0) {
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        sum[r] = F::mul(F::codes(w[d][r][s]), xf, s % (4 / GP) == 0 ? (q4_f4){0.0f, 0.0f, 0.0f, 0.0f} : sum[r]);
-                        if ((s + 1) % (4 / GP) == 0) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[r][e] = fmaf(sc[d][r][s / (4 / GP)][e], sum[r][e], acc[r][e]);
-                        }
+                        for (int e = 0; e < 4; ++e) acc[e] = fmaf((float)sc[d][s / (4 / GP)][e], sum[e], acc[e]);
                     }
                 }
                 codes(d, c + D);
@@ -299,26 +295,25 @@ __global__ __launch_bounds__(512) void q4_columns_kernel(const Q4Args a) {
             }
         }
     }
-    q4_f4* part = (q4_f4*)q4_smem;       // [wave][r][lane]
-#pragma unroll
-    for (int r = 0; r < RT; ++r) part[(wave * RT + r) * 64 + lane] = acc[r];
+    q4_f4* part = (q4_f4*)q4_smem;       // [wave][lane]
+    part[wave * 64 + lane] = acc;
     __syncthreads();
-    for (int i = tid; i < RT * 4 * a.n; i += (int)blockDim.x) {
-        const int r = i & (RT - 1), gg = (i / RT) & 3, token = i / (RT * 4);
+    for (int i = tid; i < 4 * a.n; i += (int)blockDim.x) {
+        const int gg = i & 3, token = i >> 2;
         q4_f4 v = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int k = 0; k < waves; ++k)
-            for (int p = P - 1; p >= 0; --p) v += part[(k * RT + r) * 64 + gg * 16 + token * P + p];
-        q4_store<T>(a, token, (tile0 + r) * 16 + 4 * gg, v);
+            for (int p = P - 1; p >= 0; --p) v += part[k * 64 + gg * 16 + token * P + p];
+        q4_store<T>(a, token, tile * 16 + 4 * gg, v);
     }
 }
 
-template <typename T, int GP, int RT>
+template <typename T, int GP>
 hipError_t launch_columns(const Q4Args& a, hipStream_t s) {
-    const int tiles = (a.cout + 15) / 16, waves = a.blocks >= 8 ? 8 : a.blocks;
+    const int waves = a.blocks >= 8 ? 8 : a.blocks;
     const size_t lds = (size_t)waves * 8192;
-    const dim3 grid((unsigned)((tiles + RT - 1) / RT));
-    if (a.n <= 4) CADNN_LAUNCH((q4_columns_kernel<T, GP, RT, 1>), grid, dim3(64u * waves), lds, s, a);
-    else CADNN_LAUNCH((q4_columns_kernel<T, GP, RT, Q4Frag<T>::kParts == 3 ? 2 : 4>), grid, dim3(64u * waves), lds, s, a);
+    const dim3 grid((unsigned)((a.cout + 15) / 16));
+    if (a.n <= 4) CADNN_LAUNCH((q4_columns_kernel<T, GP, 1>), grid, dim3(64u * waves), lds, s, a);
+    else CADNN_LAUNCH((q4_columns_kernel<T, GP, Q4Frag<T>::kParts == 3 ? 2 : 4>), grid, dim3(64u * waves), lds, s, a);
     return hipGetLastError();
 }
 
@@ -555,15 +550,10 @@ hipError_t launch_q4(const Q4Args& a, hipStream_t s) {
             if (fills(64, 32, 256)) return launch_few<T, GP, 4, 2>(a, s);
         }
     }
-    // Staged activations pay from rows of some length on (one token, 512 -> 512: fp16 3.5 staged, 2.9 not; 4096 -> 4096: 5.0, 5.9), two
-    // tiles of filters to a wave where it has activations to cut apart (fp32, 5 tokens, 8192 -> 8192: 17.1 one, 15.3 two).
-    const bool two = fills(32, 16, 256) && a.blocks > 8;
-    if constexpr (sizeof(T) == 2) {
-        if (a.blocks > 16 && a.n <= 16) return launch_columns<T, GP, 1>(a, s);
-    } else {
-        if (a.blocks > 8 && a.n <= 5) return two ? launch_columns<T, GP, 2>(a, s) : launch_columns<T, GP, 1>(a, s);
-    }
-    if (a.n <= 16) return two ? launch_few<T, GP, 2, 1>(a, s) : launch_few<T, GP, 1, 1>(a, s);
+    // Staged activations pay from rows of some length on (one token, 512 -> 512: fp16 3.5 staged, 2.9 not; 4096 -> 4096: 5.0, 5.9).
+    if (a.n <= 16 / Q4Frag<T>::kParts && a.blocks > (sizeof(T) == 2 ? 16 : 8)) return launch_columns<T, GP>(a, s);
+    // (13 tokens, 5003 -> 4099, fp16: one tile of filters a wave 24.6, two 15.8; 4096 filters 14.6, 15.9)
+    if (a.n <= 16) return a.cout > 16 * 256 && a.blocks > 8 ? launch_few<T, GP, 2, 1>(a, s) : launch_few<T, GP, 1, 1>(a, s);
     if (fills(64, 16, 256)) return launch_few<T, GP, 4, 1>(a, s);
     if (fills(32, 16, 256)) return launch_few<T, GP, 2, 1>(a, s);
     return launch_few<T, GP, 1, 1>(a, s);
