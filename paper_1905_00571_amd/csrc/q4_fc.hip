@@ -520,43 +520,60 @@ hipError_t launch_tile(const Q4Args& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Which kernel: the largest tile that still gives every compute unit a workgroup (large tiles read and expand less, but a
-// workgroup alone on its unit waits out every latency); below that, and for few tokens, the kernels that split the inputs
-// over a workgroup's waves.  us on random data, 4096 -> 4096, groups of 128, fp16: 64 tokens 11.5 (few), 12.8 (64 x 32 tiles);
-// 128 tokens 17.1, 13.6; 512 tokens 29.7 (64 x 32), 25.2 (128 x 64), 53 (128 x 128); 2048 tokens 78 (128 x 64), 76 (128 x 128), and with
-// groups of 32 130 and 98.  fp32, 512 tokens: 82 (few), 59 (128 x 32), 55 (256 x 32), 94 (256 x 64); 2048 tokens: 216 (256 x 32), 200 (256 x 64).
+// What a kernel takes, in us for rows of 4096 inputs, from the number of its workgroups: `one` while every compute unit has at
+// most one, then `full` for every `fit` of them, the last ones included, which run `fit` at a time -- or, small as they are
+// (1024 to a round), for as many as there are.
+struct Q4Cost {
+    double one, full;
+    int fit;
+    double of(int64_t workgroups) const {
+        if (workgroups <= 256) return one;
+        return fit >= 1024 ? std::max(one, full * (double)workgroups / fit) : full * (double)((workgroups + fit - 1) / fit);
+    }
+};
+
+// Which kernel.  Large tiles read and expand less, but a workgroup alone on its compute unit waits out every latency, and one
+// more than fit costs a round; so the kernels are compared by what they were measured to take (random data, 4096 -> 4096, 33 to 2048
+// tokens; groups of 128, 64, 32).  fp16, 128 x 128 / 128 x 64 / 64 x 32 tiles / few tokens: 128 tokens 53, 23, 13.6, 17; 512 tokens 53,
+// 25, 30, 55; 2048 tokens 76, 78, 108, more.  fp32, 256 x 64 / 256 x 32 / 128 x 32 / few tokens: 128 tokens 92, 52, 38, 23; 512 tokens 94, 55, 59, 82;
+// 2048 tokens 200, 216, 218, more.
 template <typename T, int GP>
 hipError_t launch_q4(const Q4Args& a, hipStream_t s) {
-    auto fills = [&](int filters, int tokens, int workgroups) {
-        return (int64_t)((a.cout + filters - 1) / filters) * ((a.n + tokens - 1) / tokens) >= workgroups;
-    };
+    auto workgroups = [&](int filters, int tokens) { return (int64_t)((a.cout + filters - 1) / filters) * ((a.n + tokens - 1) / tokens); };
     if (a.n > 32) {
+        constexpr int G = GP == 1 ? 0 : GP == 2 ? 1 : 2;
         if constexpr (sizeof(T) == 2) {
             // straight to LDS: whole pieces of eight, and 32-bit offsets from the first token of a tile on
             const bool direct = (uintptr_t)a.x % 16 == 0 && a.x_stride % 8 == 0 && a.cin % 8 == 0 && a.x_stride < (1 << 22);
-            if (direct) {
-                if (fills(128, 128, 512)) return launch_tile<T, GP, 2, 128, GP == 1 ? 4 : 2, 1, true>(a, s);
-                if (fills(128, 64, 256)) return launch_tile<T, GP, 2, 64, 4, 2, true>(a, s);
-                if (fills(64, 32, 256)) return launch_tile<T, GP, 1, 32, 4, 2, true>(a, s);
-            } else {
-                if (fills(128, 64, 1024)) return launch_tile<T, GP, 2, 64, 4, 1, false>(a, s);
-                if (fills(128, 64, 256)) return launch_tile<T, GP, 2, 64, 4, 2, false>(a, s);
-                if (fills(64, 32, 256)) return launch_tile<T, GP, 1, 32, 4, 2, false>(a, s);
-            }
+            constexpr Q4Cost large[3] = {{52, 75, 512}, {52, 83, 512}, {70, 97, 512}}, middle[3] = {{24, 38, 512}, {25, 52, 512}, {36, 65, 512}};
+            constexpr Q4Cost small[3] = {{14, 28, 1024}, {15, 30, 1024}, {18, 37, 1024}}, few[3] = {{11.5, 17, 512}, {12.5, 18.5, 512}, {14, 21, 512}};
+            constexpr Q4Cost large_in_registers[3] = {{38, 45, 512}, {40, 55, 512}, {54, 75, 512}};
+            const double l = direct ? large[G].of(workgroups(128, 128)) : large_in_registers[G].of(workgroups(128, 64));
+            const double m = (direct ? 1.0 : 1.15) * middle[G].of(workgroups(128, 64)), sm = (direct ? 1.0 : 1.15) * small[G].of(workgroups(64, 32));
+            const double f = few[G].of(workgroups(64, 16));
+            if (l <= m && l <= sm && l <= f)
+                return direct ? launch_tile<T, GP, 2, 128, GP == 1 ? 4 : 2, 1, true>(a, s) : launch_tile<T, GP, 2, 64, 4, 1, false>(a, s);
+            if (m <= sm && m <= f) return direct ? launch_tile<T, GP, 2, 64, 4, 2, true>(a, s) : launch_tile<T, GP, 2, 64, 4, 2, false>(a, s);
+            if (sm <= f) return direct ? launch_tile<T, GP, 1, 32, 4, 2, true>(a, s) : launch_tile<T, GP, 1, 32, 4, 2, false>(a, s);
         } else {
-            if (fills(256, 64, 256)) return launch_tile<T, GP, 4, 64, 2, 2, false>(a, s);
-            if (fills(256, 32, 256)) return launch_tile<T, GP, 4, 32, 4, 2, false>(a, s);
-            if (fills(128, 32, 256)) return launch_tile<T, GP, 2, 32, 4, 2, false>(a, s);
-            if (fills(64, 32, 256)) return launch_few<T, GP, 4, 2>(a, s);
+            constexpr Q4Cost large[3] = {{93, 98, 256}, {96, 105, 256}, {106, 115, 256}}, middle[3] = {{52, 54, 256}, {54, 57, 256}, {59, 60, 256}};
+            constexpr Q4Cost small[3] = {{38, 29, 256}, {39, 31, 256}, {41, 37, 256}}, few[3] = {{23, 21, 256}, {25, 23, 256}, {28.5, 26, 256}};
+            const double l = large[G].of(workgroups(256, 64)), m = middle[G].of(workgroups(256, 32)), sm = small[G].of(workgroups(128, 32));
+            const double f = few[G].of(workgroups(64, 32));
+            if (l <= m && l <= sm && l <= f) return launch_tile<T, GP, 4, 64, 2, 2, false>(a, s);
+            if (m <= sm && m <= f) return launch_tile<T, GP, 4, 32, 4, 2, false>(a, s);
+            if (sm <= f) return launch_tile<T, GP, 2, 32, 4, 2, false>(a, s);
+            if (workgroups(64, 32) >= 256) return launch_few<T, GP, 4, 2>(a, s);
         }
     }
     // Staged activations pay from rows of some length on (one token, 512 -> 512: fp16 3.5 staged, 2.9 not; 4096 -> 4096: 5.0, 5.9).
     if (a.n <= 16 / Q4Frag<T>::kParts && a.blocks > (sizeof(T) == 2 ? 16 : 8)) return launch_columns<T, GP>(a, s);
     // (13 tokens, 5003 -> 4099, fp16: one tile of filters a wave 24.6, two 15.8; 4096 filters 14.6, 15.9)
     if (a.n <= 16) return a.cout > 16 * 256 && a.blocks > 8 ? launch_few<T, GP, 2, 1>(a, s) : launch_few<T, GP, 1, 1>(a, s);
-    if (fills(64, 16, 256)) return launch_few<T, GP, 4, 1>(a, s);
-    if (fills(32, 16, 256)) return launch_few<T, GP, 2, 1>(a, s);
-    return launch_few<T, GP, 1, 1>(a, s);
+    constexpr bool h = sizeof(T) == 2;
+    constexpr Q4Cost few1 = {h ? 7.3 : 11.3, h ? 12.5 : 20, 512}, few2 = {h ? 9.3 : 11.8, h ? 13 : 21.5, 512}, few4 = {h ? 11.5 : 15.2, h ? 17.0 : 29, 512};
+    const double f1 = few1.of(workgroups(16, 16)), f2 = few2.of(workgroups(32, 16)), f4 = few4.of(workgroups(64, 16));
+    return f4 <= f2 && f4 <= f1 ? launch_few<T, GP, 4, 1>(a, s) : f2 <= f1 ? launch_few<T, GP, 2, 1>(a, s) : launch_few<T, GP, 1, 1>(a, s);
 }
 
 template <typename T>
