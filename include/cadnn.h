@@ -393,6 +393,9 @@ cadnn_status cadnn_net_add_global_avgpool(cadnn_net* net, int src_buf, int dst_b
 cadnn_status cadnn_net_add_concat(cadnn_net* net, const int* src_bufs, int count, int dst_buf);
 cadnn_status cadnn_net_add_fc(cadnn_net* net, const cadnn_weights* w, const void* bias_dev,
                               int relu, int src_buf, int dst_buf);
+/* The same layer with 4-bit weights (cadnn_q4_fc, of the net's type); its variant name is "q4fc". */
+cadnn_status cadnn_net_add_q4_fc(cadnn_net* net, const cadnn_q4_weights* w, const void* bias_dev,
+                                 int relu, int src_buf, int dst_buf);
 /* Size of the workspace cadnn_net_finalize needs.  It depends on the layout flags below
  * (CADNN_NET_PLAIN_LAYOUT, CADNN_NET_NO_FUSION): the value is for flags 0 unless
  * cadnn_net_op_info has been called with other flags since the last op was added; finalize
@@ -506,7 +509,7 @@ cadnn_status cadnn_net_profile(cadnn_net* net, const void* x, void* y, void* str
  * `repeats` passes; 0 for ops that launch nothing.  Synchronises the stream. */
 cadnn_status cadnn_net_profile_in_order(cadnn_net* net, const void* x, void* y, void* stream, int repeats,
                                         float* ms_per_op);
-/* Name of the kernel serving op `op_index` (a conv variant name, "dwconv", "sfc", "maxpool",
+/* Name of the kernel serving op `op_index` (a conv variant name, "dwconv", "sfc", "q4fc", "maxpool",
  * "avgpool2d", "avgpool", "concat", or "fused" / "in place" for an op that launches nothing),
  * NUL-terminated into buf. */
 cadnn_status cadnn_net_op_variant(const cadnn_net* net, int op_index, char* buf, size_t len);

@@ -120,6 +120,7 @@ def lib() -> ctypes.CDLL:
         "cadnn_net_add_avgpool": (_i, [_vp, _i, _i, _i, _i, _i]),
         "cadnn_net_add_concat": (_i, [_vp, ctypes.POINTER(_i), _i, _i]),
         "cadnn_net_add_fc": (_i, [_vp, _vp, _vp, _i, _i, _i]),
+        "cadnn_net_add_q4_fc": (_i, [_vp, _vp, _vp, _i, _i, _i]),
         "cadnn_net_workspace_bytes": (_i, [_vp, ctypes.POINTER(ctypes.c_size_t)]),
         "cadnn_net_finalize": (_i, [_vp, _vp, ctypes.c_size_t, _i]),
         "cadnn_net_op_info": (_i, [_vp, _i, _i, ctypes.POINTER(OpInfo)]),
@@ -787,7 +788,9 @@ def _add_ops(L, handle, ops, weights, biases, input_shape, dtype, keep, to_devic
     shapes = {0: tuple(input_shape)}
     for i, op in enumerate(ops):
         if op.kind in ("conv", "fc", "dwconv"):
-            pw = cadnn_pack_weights(np.asarray(weights[i], dtype=np.float32), dtype)
+            # (a fully connected op's weights may be a handle of 4-bit weights: Q4Weights)
+            q4 = op.kind == "fc" and isinstance(weights[i], Q4Weights)
+            pw = weights[i] if q4 else cadnn_pack_weights(np.asarray(weights[i], dtype=np.float32), dtype)
             b = None
             if to_device is not None and biases[i] is not None:
                 b = to_device(biases[i])
@@ -805,7 +808,8 @@ def _add_ops(L, handle, ops, weights, biases, input_shape, dtype, keep, to_devic
                 shapes[op.dst] = (s[0], s[1], _out_size(s[2], pw.kh, op.stride, op.pad),
                                   _out_size(s[3], pw.kw, op.stride, op.pad))
             else:
-                _check(L.cadnn_net_add_fc(handle, pw.handle, _dptr(b), int(bool(op.relu)), op.src, op.dst))
+                add = L.cadnn_net_add_q4_fc if q4 else L.cadnn_net_add_fc
+                _check(add(handle, pw.handle, _dptr(b), int(bool(op.relu)), op.src, op.dst))
                 shapes[op.dst] = (shapes[op.src][0], pw.cout, 1, 1)
         elif op.kind == "maxpool":
             _check(L.cadnn_net_add_maxpool(handle, op.k, op.stride, op.pad, op.src, op.dst))
@@ -866,7 +870,8 @@ def build_net(ops: Sequence, weights: Sequence, biases: Sequence, input_shape, d
     (CADNN_NET_STATIC_WORKSPACE), which is what Net.run_noalloc needs.
 
     `ops` are records with .kind in {"conv", "dwconv", "fc", "maxpool", "avgpool2d", "avgpool", "concat"} and
-    .src/.dst/.res/.k/.stride/.pad/.relu fields (see workloads.nets.Op).
+    .src/.dst/.res/.k/.stride/.pad/.relu fields (see workloads.nets.Op).  An "fc" op's weights may be a
+    Q4Weights handle of the net's type: the layer then runs with 4-bit weights.
     """
     import torch
     L = lib()

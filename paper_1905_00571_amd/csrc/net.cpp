@@ -643,7 +643,7 @@ cadnn_status launch_one(cadnn_net* net, size_t i, const void* x, void* y, hipStr
             return launch_depthwise(op.w, src, op.xd, dst, op.yd, op.in.n, op.stride, op.pad, (const float*)op.bias,
                                     op.relu, s);
         case OP_FC:
-            return launch_fc(op.w, src, dst, op.in.n, (const float*)op.bias, op.relu, s);
+            return launch_fc_op(op, src, dst, s);
         case OP_MAXPOOL:
             return launch_maxpool(src, op.xd, dst, op.yd, op.in.n, op.k, op.stride, op.pad, net->dtype, s);
         case OP_AVGPOOL2D:
@@ -938,6 +938,26 @@ extern "C" cadnn_status cadnn_net_add_fc(cadnn_net* net, const cadnn_weights* w,
     return CADNN_OK;
 }
 
+extern "C" cadnn_status cadnn_net_add_q4_fc(cadnn_net* net, const cadnn_q4_weights* w, const void* bias, int relu, int src, int dst) try {
+    if (!net || !w) return fail(CADNN_EINVAL, "cadnn_net_add_q4_fc: NULL pointer");
+    if (net->finalized) return fail(CADNN_EINVAL, "cadnn_net_add_q4_fc: net already finalized");
+    if (w->dtype != net->dtype) return fail(CADNN_EINVAL, "cadnn_net_add_q4_fc: dtype of weights and net differ");
+    if (src == dst) return fail(CADNN_EINVAL, "cadnn_net_add_q4_fc: dst aliases src");
+    NetOp op;
+    cadnn_status st = src_shape(net, src, &op.in, &op.src_inst);
+    if (st != CADNN_OK) return st;
+    if ((size_t)op.in.c * op.in.h * op.in.w != (size_t)w->cin)
+        return fail(CADNN_EINVAL, "cadnn_net_add_q4_fc: %zu input features, weights take %d",
+                    (size_t)op.in.c * op.in.h * op.in.w, w->cin);
+    op.out = Shape{op.in.n, w->cout, 1, 1};
+    op.kind = OP_FC; op.q4 = w; op.bias = bias; op.relu = relu; op.src = src; op.dst = dst;
+    if ((st = note_output(net, dst, op.out)) != CADNN_OK) return st;
+    net->ops.push_back(op);
+    return CADNN_OK;
+} catch (const std::bad_alloc&) {
+    return fail(CADNN_ENOMEM, "cadnn_net_add_q4_fc: out of host memory");
+}
+
 extern "C" cadnn_status cadnn_net_workspace_bytes(const cadnn_net* net, size_t* bytes) try {
     if (!net || !bytes) return fail(CADNN_EINVAL, "cadnn_net_workspace_bytes: NULL pointer");
     if (net->ops.empty()) return fail(CADNN_EINVAL, "cadnn_net_workspace_bytes: empty net");
@@ -1015,7 +1035,7 @@ static cadnn_status prepare_planes(cadnn_net* net) {
         ConvExtra ex;
         if (op.kind == OP_CONV && op.fused_into < 0)
             st = conv2d_prepare_impl(eff_w(net, op), op.xd, op.in.n, op.stride, op.pad, out_s2d(op), shortcut_geom(net, op, &ex));
-        if (op.kind == OP_FC) st = cadnn_fc_prepare(op.w);
+        if (op.kind == OP_FC) st = prepare_fc_op(op);
         if (op.kind == OP_DEPTHWISE) st = ensure_dw_device(op.w);
         if (st != CADNN_OK) return st;
     }
@@ -1372,7 +1392,7 @@ extern "C" cadnn_status cadnn_net_op_variant(const cadnn_net* net, int op_index,
                                                                  shortcut_geom(net, op, &ex));
             break;
         }
-        case OP_FC: name = "sfc"; break;
+        case OP_FC: name = op.q4 ? "q4fc" : "sfc"; break;
         case OP_DEPTHWISE: name = op.fused_into >= 0 ? "fused" : "dwconv"; break;
         case OP_MAXPOOL: name = op.fused_into >= 0 ? "fused" : "maxpool"; break;
         case OP_AVGPOOL: name = op.fused_into >= 0 ? "fused" : "avgpool"; break;

@@ -2,6 +2,7 @@
 #pragma once
 
 #include "channels_last.h"
+#include "q4.h"
 
 namespace cadnn {
 
@@ -19,6 +20,7 @@ struct Shape {
 struct NetOp {
     OpKind kind;
     const cadnn_weights* w = nullptr;
+    const cadnn_q4_weights* q4 = nullptr;    // fully connected layer with 4-bit weights (w is NULL)
     const void* bias = nullptr;
     int stride = 1, pad = 0, relu = 0, k = 0;
     int src = 0, dst = 0, res = -1;          // buffer ids as given by the caller
@@ -133,6 +135,9 @@ namespace cadnn {
 std::unique_ptr<ClNet> cl_layout(const cadnn_net* net);
 bool cl_expected_faster(const cadnn_net* net);
 cadnn_status cl_prepare(cadnn_net* net);
+// The device layout of a fully connected op's weights, and its launch on rows that follow each other.
+cadnn_status prepare_fc_op(const NetOp& op);
+cadnn_status launch_fc_op(const NetOp& op, const void* src, void* dst, hipStream_t s);
 cadnn_status cl_launch_one(cadnn_net* net, size_t i, const void* x, void* y, hipStream_t s);
 cadnn_status cl_tune(cadnn_net* net, const void* x, void* y, hipStream_t s);
 void cl_op_info(const cadnn_net* net, size_t i, cadnn_op_info* out);

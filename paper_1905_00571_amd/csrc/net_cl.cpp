@@ -283,6 +283,15 @@ bool cl_expected_faster(const cadnn_net* net) {
            0.77 * (4.5 * planes_launches + nonzero / 8.5e6);
 }
 
+cadnn_status prepare_fc_op(const NetOp& op) {
+    return op.q4 ? ensure_q4_device(op.q4, "cadnn_net_finalize", nullptr, false) : cadnn_fc_prepare(op.w);
+}
+
+cadnn_status launch_fc_op(const NetOp& op, const void* src, void* dst, hipStream_t s) {
+    if (!op.q4) return launch_fc(op.w, src, dst, op.in.n, (const float*)op.bias, op.relu, s);
+    return launch_q4_fc(op.q4, src, op.q4->cin, dst, op.q4->cout, op.in.n, (const float*)op.bias, op.relu ? CADNN_ACT_RELU : CADNN_ACT_NONE, s);
+}
+
 cadnn_status cl_prepare(cadnn_net* net) {
     const size_t e = net->elem();
     std::vector<char> image;
@@ -290,7 +299,7 @@ cadnn_status cl_prepare(cadnn_net* net) {
         const NetOp& op = net->ops[i];
         ClOp& c = *net->cl->ops[i];
         cadnn_status st = CADNN_OK;
-        if (op.kind == OP_FC) st = cadnn_fc_prepare(op.w);
+        if (op.kind == OP_FC) st = prepare_fc_op(op);
         if (op.kind == OP_DEPTHWISE && !c.dw.p) {
             try {
                 std::vector<float> taps((size_t)op.w->cout * 9, 0.0f);
@@ -342,7 +351,7 @@ cadnn_status cl_launch_one(cadnn_net* net, size_t i, const void* x, void* y, hip
             st = launch_cl_depthwise((const float*)c.dw.p, src, c.xd, dst, c.yd, op.out.n, op.stride, op.pad, (const float*)op.bias, op.relu, f16, s);
             break;
         case OP_FC:
-            return launch_fc(op.w, op.src_inst < 0 ? x : src, dst, op.in.n, (const float*)op.bias, op.relu, s);
+            return launch_fc_op(op, op.src_inst < 0 ? x : src, dst, s);
         case OP_MAXPOOL:
         case OP_AVGPOOL2D:
             st = launch_cl_pool(src, c.xd, dst, c.yd, c.flat, op.out.n, op.k, op.stride, op.pad, op.kind == OP_MAXPOOL ? 0 : 1, f16, s);
@@ -436,7 +445,7 @@ const char* cl_op_variant(const cadnn_net* net, size_t i) {
     const ClOp& c = *net->cl->ops[i];
     switch (op.kind) {
         case OP_CONV: return c.fused_into >= 0 ? "fused" : c.v->name;
-        case OP_FC: return "sfc";
+        case OP_FC: return op.q4 ? "q4fc" : "sfc";
         case OP_DEPTHWISE: return "dwconv";
         case OP_MAXPOOL: return "maxpool";
         case OP_AVGPOOL: return "avgpool";

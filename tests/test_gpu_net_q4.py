@@ -1,0 +1,106 @@
+"""Nets whose fully connected layers have 4-bit weights (cadnn_net_add_q4_fc), on plane and channels-last tensors, replayed as a
+graph and in the library's static workspace; against the oracle on the weights that the codes and scales stand for."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import workloads as wl
+import paper_1905_00571_amd as cad
+from util import assert_net_close, TOL_F16, TOL_F32
+
+
+def small_net(sparsity):
+    return [wl.Op("conv", "a", 0, 1, 16, 32, 3, 1, 1, sparsity, True), wl.Op("maxpool", "p", 1, 2, k=2, stride=2),
+            wl.Op("conv", "b", 2, 3, 32, 64, 1, 1, 0, sparsity, True), wl.Op("avgpool", "gap", 3, 4),
+            wl.Op("fc", "fc1", 4, 5, 64, 100, sparsity=0.0, relu=True), wl.Op("fc", "fc2", 5, 6, 100, 10, sparsity=0.5, relu=False)]
+
+
+def flat_net():
+    """The classifier reads a feature map, as VGG-16's does."""
+    return [wl.Op("conv", "a", 0, 1, 16, 24, 3, 1, 1, 0.8, True), wl.Op("maxpool", "p", 1, 2, k=2, stride=2),
+            wl.Op("fc", "fc1", 2, 3, 24 * 7 * 7, 130, sparsity=0.0, relu=True), wl.Op("fc", "fc2", 3, 4, 130, 40, sparsity=0.0, relu=False)]
+
+
+def quantised(ops, ws, names, group, flag):
+    """The weights with the named layers as handles, and with the values that those stand for."""
+    mixed, plain = list(ws), list(ws)
+    for i, op in enumerate(ops):
+        if op.kind == "fc" and op.name in names:
+            mixed[i] = cad.cadnn_q4_pack(np.asarray(ws[i], np.float32).reshape(op.cout, op.cin), group, flag)
+            plain[i] = cad.cadnn_q4_unpack(mixed[i]).reshape(np.asarray(ws[i]).shape)
+    return mixed, plain
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("name,shape", [("small", (1, 16, 14, 14)), ("small", (5, 16, 14, 14)), ("small", (40, 16, 28, 28)), ("flat", (1, 16, 14, 14)), ("flat", (3, 16, 14, 14))])
+@pytest.mark.parametrize("quant", [("fc1", "fc2"), ("fc1",)])
+def test_net_with_4bit_classifier(dtype, name, shape, quant):
+    flag, tol = (cad.F16, TOL_F16) if dtype == "f16" else (cad.F32, TOL_F32)
+    ops = small_net(0.8) if name == "small" else flat_net()
+    x, ws, bs = wl.net_tensors(ops, "q4net-" + name, shape, input_relu=True)
+    mixed, plain = quantised(ops, ws, quant, 32, flag)
+    ref, _, _ = oracle.run_net(ops, x, plain, bs)
+    xd = torch.from_numpy(x).cuda()
+    xd = xd.half() if flag == cad.F16 else xd
+    for options in ({"use_graph": True}, {"use_graph": False, "fuse": False, "plain_layout": True}, {"static_workspace": True, "use_graph": False}):
+        net = cad.build_net(ops, mixed, bs, shape, flag, **options)
+        names = net.variants()
+        assert [names[i] for i, op in enumerate(ops) if op.kind == "fc"] == ["q4fc" if op.name in quant else "sfc" for op in ops if op.kind == "fc"]
+        for _ in range(3):
+            y = net.run_noalloc(xd, torch.empty(net.out_shape, dtype=xd.dtype, device="cuda")) if "static_workspace" in options else net.run(xd)
+            assert_net_close(y.float().cpu().numpy().reshape(ref.shape), ref, tol, str(options))
+        net.free()
+    for w in mixed:
+        if isinstance(w, cad.Q4Weights):
+            w.free()
+
+
+@pytest.mark.gpu
+def test_4bit_classifier_on_channels_last_tensors():
+    """A net that is taken to channels-last tensors (by pinning a convolution) runs its 4-bit layers there as well."""
+    ops = small_net(0.5)
+    shape = (8, 16, 28, 28)
+    x, ws, bs = wl.net_tensors(ops, "q4net-cl", shape, input_relu=True)
+    mixed, plain = quantised(ops, ws, ("fc1",), 64, cad.F16)
+    ref, _, _ = oracle.run_net(ops, x, plain, bs)
+    net = cad.build_net(ops, mixed, bs, shape, cad.F16)
+    if not net.op_variant(0).startswith("cl_"):
+        names = [n for n in net.op_candidates(0) if n.startswith("cl_")]
+        if names:
+            net.set_op_variant(0, names[0])
+    for k in range(2):
+        y = net.run(torch.from_numpy(x).cuda().half())
+        assert_net_close(y.float().cpu().numpy().reshape(ref.shape), ref, TOL_F16)
+    assert net.op_variant(4) == "q4fc"
+    net.free()
+
+
+def test_net_with_4bit_layer_is_planned_and_checked_without_a_gpu():
+    ops = small_net(0.8)
+    shape = (2, 16, 14, 14)
+    _, ws, _ = wl.net_tensors(ops, "q4net-plan", shape, input_relu=True)
+    mixed, _ = quantised(ops, ws, ("fc1", "fc2"), 32, cad.F32)
+    infos, nbytes = cad.plan_net(ops, mixed, shape)
+    want, same = cad.plan_net(ops, ws, shape)
+    assert infos == want and nbytes == same                  # the layout does not depend on how a layer keeps its weights
+    L = cad.lib()
+    net = ctypes.c_void_p()
+    h16 = cad.cadnn_q4_pack(np.ones((4, 64), np.float32), 32, cad.F16)
+    h = cad.cadnn_q4_pack(np.ones((4, 64), np.float32), 32, cad.F32)
+    assert L.cadnn_net_create(0, 1, 4, 4, 4, ctypes.byref(net)) == 0
+    assert L.cadnn_net_add_q4_fc(None, h.handle, None, 0, 0, 1) == 1
+    assert L.cadnn_net_add_q4_fc(net, None, None, 0, 0, 1) == 1
+    assert L.cadnn_net_add_q4_fc(net, h16.handle, None, 0, 0, 1) == 1 and b"dtype" in L.cadnn_last_error()
+    assert L.cadnn_net_add_q4_fc(net, h.handle, None, 0, 0, 0) == 1
+    assert L.cadnn_net_add_q4_fc(net, h.handle, None, 0, 3, 1) == 1                  # reads an unwritten buffer
+    assert L.cadnn_net_add_q4_fc(net, h.handle, None, 0, 0, 1) == 0                  # 4 x 4 x 4 features
+    assert L.cadnn_net_add_q4_fc(net, h.handle, None, 0, 1, 2) == 1 and b"features" in L.cadnn_last_error()
+    n = ctypes.c_int()
+    assert L.cadnn_net_num_ops(net, ctypes.byref(n)) == 0 and n.value == 1
+    assert L.cadnn_net_free(net) == 0
+    for w in [h, h16] + [m for m in mixed if isinstance(m, cad.Q4Weights)]:
+        w.free()
