@@ -244,11 +244,13 @@ cadnn_status cadnn_causal_conv1d(const cadnn_weights* w, const void* x, int64_t 
  * sequences that are too few to fill the chip are cut into pieces that run side by side.  Without it, or with
  * less, every sequence is worked on from end to end: slower, and with differently rounded sums.
  * Errors: EINVAL (NULL pointer, bad sizes or strides as above, channels that are no multiple of groups, a
- * misaligned pointer, unknown dtype); EUNSUPPORTED (dstate above 256, more than 2^20 channels, 4096 groups, 65535 sequences or
+ * misaligned pointer, unknown dtype, negative longest); EUNSUPPORTED (dstate above 256, more than 2^20 channels, 4096 groups, 65535 sequences or
  * 2^30 tokens); EHIP. */
 typedef struct cadnn_scan_args {
     cadnn_dtype dtype;
     int tokens, seqs, channels, dstate, groups, softplus;
+    int longest;                 /* rows of the longest sequence, 0 where it is not known: a hint (with seq_start) on how to divide
+                                    the work, any value gives the same results but for rounding */
     const int32_t* seq_start;
     const void *x, *dt, *b, *c, *z;
     void* y;

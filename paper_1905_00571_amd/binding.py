@@ -53,7 +53,7 @@ class PlanInfo(ctypes.Structure):
 class ScanArgs(ctypes.Structure):
     """Mirror of cadnn_scan_args."""
     _fields_ = [("dtype", ctypes.c_int), ("tokens", ctypes.c_int), ("seqs", ctypes.c_int), ("channels", ctypes.c_int),
-                ("dstate", ctypes.c_int), ("groups", ctypes.c_int), ("softplus", ctypes.c_int), ("seq_start", _vp),
+                ("dstate", ctypes.c_int), ("groups", ctypes.c_int), ("softplus", ctypes.c_int), ("longest", ctypes.c_int), ("seq_start", _vp),
                 ("x", _vp), ("dt", _vp), ("b", _vp), ("c", _vp), ("z", _vp), ("y", _vp),
                 ("x_stride", _i64), ("dt_stride", _i64), ("b_stride", _i64), ("c_stride", _i64), ("z_stride", _i64),
                 ("y_stride", _i64), ("a", _vp), ("d", _vp), ("dt_bias", _vp), ("state", _vp)]
@@ -541,7 +541,7 @@ def _i32():
     return torch.int32
 
 
-def _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, out) -> ScanArgs:
+def _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, longest, out) -> ScanArgs:
     f32, dtype, shape = _f32(), x.dtype, x.shape
     if len(shape) != 2 or (dtype is not f32 and dtype is not _torch_dtype(F16)):
         raise ValueError("x is not a float32 or float16 tensor [tokens][channels]")
@@ -553,7 +553,7 @@ def _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, 
     groups = 1 if b.dim() == 2 else b.shape[1]
     flat, grouped = (tokens, dstate), (tokens, groups, dstate)
     return ScanArgs(
-        F32 if dtype is f32 else F16, tokens, seqs, channels, dstate, groups, 1 if softplus else 0,
+        F32 if dtype is f32 else F16, tokens, seqs, channels, dstate, groups, 1 if softplus else 0, longest,
         None if seq_start is None else _whole(seq_start, "seq_start", _i32(), dev, (seqs + 1,)),
         x.data_ptr(), dt.data_ptr(), b.data_ptr(), c.data_ptr(), None if z is None else z.data_ptr(),
         None if out is None else out.data_ptr(),
@@ -567,26 +567,26 @@ def _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, 
 
 
 def cadnn_selective_scan_workspace_bytes(x, dt, a, b, c, d=None, z=None, dt_bias=None, softplus: bool = False, state=None,
-                                         seq_start=None, seqs: int = 1) -> int:
+                                         seq_start=None, seqs: int = 1, longest: int = 0) -> int:
     """Bytes of workspace with which cadnn_selective_scan works on long sequences in pieces."""
-    g = _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, None)
+    g = _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, longest, None)
     nbytes = ctypes.c_size_t()
     _check(lib().cadnn_selective_scan_workspace_bytes(ctypes.byref(g), ctypes.byref(nbytes)))
     return int(nbytes.value)
 
 
 def cadnn_selective_scan(x, dt, a, b, c, d=None, z=None, dt_bias=None, softplus: bool = False, state=None, seq_start=None,
-                         seqs: int = 1, out=None, workspace=None, stream=None):
+                         seqs: int = 1, out=None, workspace=None, stream=None, longest: int = 0):
     """x, dt, z: CUDA tensors [tokens][channels]; b, c: [tokens][groups][dstate] or [tokens][dstate]; a: [channels][dstate]; state:
     [seqs][channels][dstate], replaced.  workspace: a uint8 tensor (None: one is taken from torch's allocator for the call; an empty one:
-    no workspace)."""
+    no workspace).  longest: rows of the longest of ragged sequences, where the caller knows it (a hint)."""
     dev = _cuda_index(x)
     if not _here(dev, stream):
         with _Elsewhere(dev, stream, (x, dt, a, b, c, d, z, dt_bias, state, seq_start, out, workspace)):
-            return cadnn_selective_scan(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, out, workspace)
+            return cadnn_selective_scan(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, out, workspace, None, longest)
     if out is None:
         out = x.new_empty(x.shape)
-    g = _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, out)
+    g = _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, longest, out)
     L, ref = lib(), ctypes.byref(g)
     if workspace is None:
         nbytes = ctypes.c_size_t()

@@ -196,6 +196,9 @@ extern "C" cadnn_status cadnn_causal_conv1d(const cadnn_weights* w, const void* 
             return fail(CADNN_EINVAL, "%s: the first call uploads the weights and cannot be captured (cadnn_depthwise_prepare)", who);
     }
     if ((st = ensure_dw_device(w)) != CADNN_OK) return st;
+    int device = -1;
+    CADNN_HIP(hipGetDevice(&device));
+    if (device != w->dw_device) return fail(CADNN_EINVAL, "%s: the weights are on device %d, the current one is %d", who, w->dw_device, device);
     CcArgs a{};
     a.x = x; a.y = y; a.w = (const float*)w->d_dw.p; a.bias = (const float*)bias; a.state = w->kw > 1 ? state : nullptr;
     a.x_stride = x_stride; a.y_stride = y_stride;

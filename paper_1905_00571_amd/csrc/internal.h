@@ -462,6 +462,7 @@ struct cadnn_weights {
     // depthwise filters (cin == 1): fp32 table [cout][kh*kw], zeros where pruned
     mutable cadnn::DevBuf d_dw;
     mutable bool dw_ready = false;
+    mutable int dw_device = -1;      // the device d_dw is on
     // conv plans, built lazily
     mutable std::mutex mu;
     // (shared: a co-launch table of the net runner holds the plans its records point into)

@@ -1101,6 +1101,7 @@ cadnn_status ensure_dw_device(const cadnn_weights* w) {
         for (int r = 0; r < w->cout; ++r)
             for (int32_t i = w->row_ptr[r]; i < w->row_ptr[r + 1]; ++i)
                 table[(size_t)w->perm[r] * kk + w->col_idx[i]] = w->vals[i];
+        CADNN_HIP(hipGetDevice(&w->dw_device));
         cadnn_status st = w->d_dw.upload(table.data(), table.size() * 4);
         if (st != CADNN_OK) return st;
     } catch (const std::bad_alloc&) {

@@ -5,6 +5,8 @@
 // The codes reach the matrix instructions as what they are, small integers, exact in fp16 and bf16; a group's sum is
 // taken in fp32 and multiplied by its scale there, so that no weight is ever rounded.  fp32 activations are cut into three
 // bf16 parts that add up to them exactly (8 bits each of 24), one matrix instruction per part.
+#include <atomic>
+
 #include "q4.h"
 
 namespace cadnn {
@@ -509,12 +511,28 @@ __global__ __launch_bounds__(256 * WK, 2) void q4_tile_kernel(const Q4Args a) {
         for (int r = 0; r < RW; ++r) q4_store<T>(a, token0 + c * 16 + j, (tile0 + r) * 16 + 4 * g, acc[r][c]);
 }
 
+// More than 64 KiB of dynamic LDS have to be asked for, once for a kernel on a device.
+struct LargeLds {
+    std::atomic<bool> asked[64] = {};
+    hipError_t ask(const void* kernel, int bytes) {
+        int device = 0;
+        hipError_t e = hipGetDevice(&device);
+        if (e != hipSuccess || (device < 64 && asked[device].load(std::memory_order_acquire))) return e;
+        e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e == hipSuccess && device < 64) asked[device].store(true, std::memory_order_release);
+        return e;
+    }
+};
+
 template <typename T, int GP, int RW, int BN, int KS, int WK, bool DIRECT>
 hipError_t launch_tile(const Q4Args& a, hipStream_t s) {
     constexpr int staged = (DIRECT ? 2 : 1) * BN * 256 * Q4Frag<T>::kParts * WK, joined = WK == 2 ? 64 * RW * BN * 4 : 0;
     constexpr int lds = staged > joined ? staged : joined;
-    static const hipError_t attr = hipFuncSetAttribute((const void*)q4_tile_kernel<T, GP, RW, BN, KS, WK, DIRECT>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (attr != hipSuccess) return attr;
+    if constexpr (lds > 64 * 1024) {
+        static LargeLds large;
+        const hipError_t e = large.ask((const void*)q4_tile_kernel<T, GP, RW, BN, KS, WK, DIRECT>, lds);
+        if (e != hipSuccess) return e;
+    }
     const dim3 grid((unsigned)((a.cout + 64 * RW - 1) / (64 * RW)), (unsigned)((a.n + BN - 1) / BN));
     CADNN_LAUNCH((q4_tile_kernel<T, GP, RW, BN, KS, WK, DIRECT>), grid, dim3(256 * WK), lds, s, a);
     return hipGetLastError();

@@ -28,7 +28,7 @@ struct SsArgs {
     float* span;          // pieces: [slot][channels], the sum of the time steps
     Sequences q;
     int channels, dstate, groups, per, softplus;
-    int chunk, blocks_per_group;
+    int chunk, blocks_per_group, longest;
     int64_t slots;
 };
 
@@ -427,6 +427,7 @@ struct ScanPlan {
     int ns, lanes;            // states of a lane, lanes of a channel
     int blocks_per_group;
     int chunk;                // tokens of a piece; 0: whole sequences
+    int longest;              // tokens of the longest sequence, as far as is known
     int64_t slots;
     size_t part_bytes, bytes;
 };
@@ -439,13 +440,18 @@ ScanPlan plan_scan(const cadnn_scan_args& g) {
     while (p.ns * p.lanes < g.dstate) p.lanes *= 2;
     const int ch = 256 / p.lanes;
     p.blocks_per_group = (per + ch - 1) / ch;
+    // The longest sequence, which decides, is known where all have one length or the caller says; of ragged ones it may be any, and as
+    // one long prompt among single tokens would take a pass over whole sequences twenty times what pieces take, a quarter of the tokens
+    // is supposed to be one sequence where there are many.
     const int average = g.tokens / g.seqs;
-    p.few = average <= 4;
+    const int longest = !g.seq_start ? average : g.longest > 0 ? std::max(g.longest, average) : g.tokens < 256 ? average : std::max(average, g.tokens / 4);
+    p.longest = longest;
+    p.few = longest <= 4;
     if (p.few) return p;
     // Waves of one pass over whole sequences.  Two to a SIMD keep the vector units busy; below that, pieces are worked on
     // side by side, at the price of a first pass for the states they start from (0.7 of a whole one).
     const int64_t waves = (int64_t)g.seqs * g.groups * p.blocks_per_group * 4;
-    if (waves >= 2048 || average < 128) return p;
+    if (waves >= 2048 || longest < 128) return p;
     p.chunk = 512;
     while (p.chunk > 32 && seq_slots(g.tokens, g.seqs, g.seq_start != nullptr, p.chunk) * g.groups * p.blocks_per_group * 4 < 2048) p.chunk /= 2;
     p.slots = seq_slots(g.tokens, g.seqs, g.seq_start != nullptr, p.chunk);
@@ -460,7 +466,7 @@ hipError_t launch_scan_passes(const SsArgs& a, hipStream_t s) {
     hipError_t e = launch_scan_pass<T, NS, L, SCAN_ENDS, FULL>(a, s);
     if (e != hipSuccess) return e;
     const int64_t per_seq = (int64_t)a.channels * a.dstate;
-    if (a.q.tokens / a.q.seqs > 16 * a.chunk) CADNN_LAUNCH(scan_join_kernel, dim3((unsigned)((per_seq + 63) / 64), (unsigned)a.q.seqs), dim3(256), 0, s, a);
+    if (a.longest > 16 * a.chunk) CADNN_LAUNCH(scan_join_kernel, dim3((unsigned)((per_seq + 63) / 64), (unsigned)a.q.seqs), dim3(256), 0, s, a);
     else CADNN_LAUNCH(scan_join_few_kernel, dim3((unsigned)((per_seq + 255) / 256), (unsigned)a.q.seqs), dim3(256), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     return launch_scan_pass<T, NS, L, SCAN_PIECES, FULL>(a, s);
@@ -501,7 +507,7 @@ cadnn_status check_scan(const char* who, const cadnn_scan_args* g) {
     if (g->dtype != CADNN_F32 && g->dtype != CADNN_F16) return fail(CADNN_EINVAL, "%s: unknown dtype %d", who, (int)g->dtype);
     cadnn_status st = check_sequences(who, g->tokens, g->seqs, g->seq_start);
     if (st != CADNN_OK) return st;
-    if (g->channels <= 0 || g->dstate <= 0 || g->groups <= 0) return fail(CADNN_EINVAL, "%s: non-positive size", who);
+    if (g->channels <= 0 || g->dstate <= 0 || g->groups <= 0 || g->longest < 0) return fail(CADNN_EINVAL, "%s: non-positive size", who);
     if (g->channels % g->groups) return fail(CADNN_EINVAL, "%s: %d channels in %d groups", who, g->channels, g->groups);
     if (g->dstate > kScanMaxStates) return fail(CADNN_EUNSUPPORTED, "%s: %d states a channel (at most %d are served)", who, g->dstate, kScanMaxStates);
     if (g->channels > (1 << 20) || g->groups > 4096 || g->seqs > 65535) return fail(CADNN_EUNSUPPORTED, "%s: more than 2^20 channels, 4096 groups or 65535 sequences", who);
@@ -551,6 +557,7 @@ extern "C" cadnn_status cadnn_selective_scan(const cadnn_scan_args* args, void* 
     a.blocks_per_group = p.blocks_per_group;
     if (p.chunk > 0 && workspace && workspace_bytes >= p.bytes) {
         a.chunk = p.chunk;
+        a.longest = p.longest;
         a.slots = p.slots;
         a.part = (float*)workspace;
         a.span = (float*)((char*)workspace + p.part_bytes);

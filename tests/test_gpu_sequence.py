@@ -199,7 +199,7 @@ def run_scan(v, seq_start, seqs, softplus=True, gate=True, bias=True, skip=True,
     return y, kept
 
 
-SCAN = [([1], 1, 1, 1), ([1], 1536, 16, 1), ([1] * 5, 100, 16, 1), ([1, 0, 1, 1], 64, 64, 4), ([2, 1, 3], 20, 3, 2), ([1], 30, 256, 3), ([4], 12, 128, 1),
+SCAN = [([1] * 40 + [300] + [2] * 30, 24, 16, 1), ([1], 1, 1, 1), ([1], 1536, 16, 1), ([1] * 5, 100, 16, 1), ([1, 0, 1, 1], 64, 64, 4), ([2, 1, 3], 20, 3, 2), ([1], 30, 256, 3), ([4], 12, 128, 1),
         ([9], 5, 5, 1), ([8, 16, 24], 70, 16, 1), ([37], 300, 8, 1), ([40, 0, 11, 90], 33, 24, 3), ([100], 20, 64, 2), ([60], 18, 100, 2),
         ([50], 6, 256, 1), ([700], 64, 16, 1), ([300, 1, 0, 512, 77], 36, 16, 2), ([1100], 40, 7, 1), ([260] * 3, 260, 20, 1), ([640], 9, 130, 3)]
 
@@ -213,7 +213,7 @@ def test_selective_scan(dtype, lens, channels, dstate, groups):
     starts = starts_of(lens)
     what = f"{lens}, {channels} channels, {dstate} states, {groups} groups"
     ref, bound, last, off = scan_reference(v, starts, True, True)
-    runs = [{"seq_start": dev(starts)}, {"seq_start": dev(starts), "workspace": torch.empty(0, dtype=torch.uint8, device="cuda")}]
+    runs = [{"seq_start": dev(starts)}, {"seq_start": dev(starts), "longest": max(lens)}, {"seq_start": dev(starts), "longest": 1}, {"seq_start": dev(starts), "workspace": torch.empty(0, dtype=torch.uint8, device="cuda")}]
     if len(set(lens)) == 1:
         runs.append({"seq_start": None})
     for how in runs:
@@ -489,7 +489,7 @@ def test_selective_scan_refusals():
     assert L.cadnn_selective_scan(None, None, 0, None) == 1
     for bad in (dict(dtype=5), dict(tokens=-1), dict(seqs=0), dict(tokens=11), dict(channels=0), dict(dstate=0), dict(groups=0), dict(groups=4), dict(x=None), dict(dt=None),
                 dict(a=None), dict(b=None), dict(c=None), dict(y=None), dict(y=1 << 10), dict(y=1 << 11), dict(y=1 << 12), dict(x_stride=5), dict(dt_stride=0), dict(y_stride=5),
-                dict(b_stride=31), dict(c_stride=16), dict(z=1 << 16, z_stride=3), dict(x=1026), dict(state=1026), dict(seq_start=1025), dict(state=1 << 14)):
+                dict(b_stride=31), dict(c_stride=16), dict(z=1 << 16, z_stride=3), dict(x=1026), dict(state=1026), dict(longest=-1), dict(seq_start=1025), dict(state=1 << 14)):
         assert call(**bad) == 1, bad
     for big in (dict(dstate=257, b_stride=600, c_stride=600), dict(channels=(1 << 20) + 2, x_stride=1 << 21, dt_stride=1 << 21, y_stride=1 << 21), dict(seqs=65536, seq_start=1 << 17),
                 dict(groups=5000, channels=5000), dict(tokens=(1 << 30) + 2)):
