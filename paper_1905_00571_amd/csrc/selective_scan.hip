@@ -211,7 +211,8 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
             else if (a.z) z[u] = ss_silu(z[u]);
         }
         span += steps;
-        char* yt = (char*)a.y + t * a.y_stride * (int64_t)sizeof(T);
+        float ys[TT];
+        // (outputs are stored behind the tile: a store under a condition would part the tokens' work from each other)
         // one token: three full-rate operations a state beside the exponential and the product under it
         auto token = [&](int u) {
             const float step = dt[u], in = step * x[u];
@@ -230,21 +231,32 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
                     if (PASS != SCAN_ENDS) y = fmaf((float)cv[e], h[k], y);
                 }
             }
-            if (PASS != SCAN_ENDS) {
-                y = ss_sum<L>(y);
-                y = fmaf(dv, x[u], y);
-                if (a.z) y *= z[u];
-                if (sub == 0 && real) *(T*)(yt + lane_at) = (T)y;
-                yt += a.y_stride * (int64_t)sizeof(T);
-            }
+            ys[u] = y;
         };
         if (left >= TT) {
 #pragma unroll
             for (int u = 0; u < TT; ++u) token(u);
         } else {
 #pragma unroll
-            for (int u = 0; u < TT; ++u)
+            for (int u = 0; u < TT; ++u) {
+                ys[u] = 0.0f;
                 if (u < left) token(u);
+            }
+        }
+        if (PASS != SCAN_ENDS) {
+#pragma unroll
+            for (int u = 0; u < TT; ++u) {
+                ys[u] = fmaf(dv, x[u], ss_sum<L>(ys[u]));
+                if (a.z) ys[u] *= z[u];
+            }
+            if (sub == 0 && real) {
+                char* yt = (char*)a.y + t * a.y_stride * (int64_t)sizeof(T);
+#pragma unroll
+                for (int u = 0; u < TT; ++u) {
+                    if (u < left) *(T*)(yt + lane_at) = (T)ys[u];
+                    yt += a.y_stride * (int64_t)sizeof(T);
+                }
+            }
         }
     }
     if (real && kept && PASS != SCAN_PIECES) {
