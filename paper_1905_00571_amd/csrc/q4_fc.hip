@@ -125,16 +125,26 @@ template <typename T>
 __device__ __forceinline__ void q4_store(const Q4Args& a, int token, int o0, q4_f4 v) {
     if (token >= a.n || o0 >= a.cout) return;
     T* out = (T*)a.y + (int64_t)token * a.y_stride + o0;
-    if (a.y_vec && o0 + 4 <= a.cout) {
-        typedef T V __attribute__((ext_vector_type(4)));
-        V r;
+    const bool four = o0 + 4 <= a.cout;
+    if (a.bias) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = (T)apply_act(v[e] + (a.bias ? a.bias[o0 + e] : 0.0f), a.act);
-        *(V*)out = r;
+        for (int e = 0; e < 4; ++e)
+            if (four || o0 + e < a.cout) v[e] += a.bias[o0 + e];
+    }
+    if (a.act == CADNN_ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = apply_act(v[e], CADNN_ACT_RELU);
+    } else if (a.act == CADNN_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = apply_act(v[e], CADNN_ACT_SILU);
+    }
+    if (a.y_vec && four) {
+        typedef T V __attribute__((ext_vector_type(4)));
+        *(V*)out = (V){(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (o0 + e < a.cout) out[e] = (T)apply_act(v[e] + (a.bias ? a.bias[o0 + e] : 0.0f), a.act);
+            if (o0 + e < a.cout) out[e] = (T)v[e];
     }
 }
 
