@@ -60,13 +60,14 @@ template <> struct Q4Frag<float> {
     // (codes as sixteenths: what the conversion of a signed nibble gives; the scales on the device are 16 times theirs)
     static __device__ __forceinline__ V codes(uint32_t w) {
         w ^= 0x88888888u;
+        const uint32_t v = w >> 4;
         union { V v8; uint32_t u[4]; } r;
+        // (a byte of w or of w >> 4 is selected by the conversion itself, which looks at its low four bits)
+        auto code = [&](int nibble) {
+            return __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)__builtin_amdgcn_ubfe(nibble & 1 ? v : w, 4 * (nibble & ~1), 8)));
+        };
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const uint32_t lo = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(w >> (4 * t))));
-            const uint32_t hi = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(w >> (16 + 4 * t))));
-            r.u[t] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
-        }
+        for (int t = 0; t < 4; ++t) r.u[t] = __builtin_amdgcn_perm(code(4 + t), code(t), 0x07060302u);
         return r.v8;
     }
     // The parts are cut off, not rounded, so that a large value's first part stays finite; what is left of an infinity
@@ -117,6 +118,19 @@ __device__ __forceinline__ void q4_load_x(const T* row, int i0, int cin, bool re
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = real && i0 + e < cin ? row[i0 + e] : (T)0.0f;
+    }
+}
+
+// The same where the row is known to reach that far.
+template <typename T>
+__device__ __forceinline__ void q4_load_whole(const T* at, T (&v)[8]) {
+    constexpr int N = 16 / (int)sizeof(T);
+    typedef T V __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+#pragma unroll
+    for (int k = 0; k < 8; k += N) {
+        const V p = *(const V*)(at + k);
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[k + e] = p[e];
     }
 }
 
@@ -251,7 +265,11 @@ __global__ __launch_bounds__(512, sizeof(T) == 4 && GP == 4 && HELD > 1 ? 2 : 4)
 #pragma unroll
         for (int k = 0; k < HELD; ++k) {
             const int i = k * 64 * waves + tid, token = i / per_token, r = i - token * per_token;
-            if (token < a.n) q4_load_x<T>(x + (int64_t)token * a.x_stride, chunk * waves * 128 + r * 8, whole ? 1 << 30 : a.cin, true, held[k]);
+            if (token < a.n) {
+                const T* from = x + (int64_t)token * a.x_stride;
+                if (whole) q4_load_whole<T>(from + chunk * waves * 128 + r * 8, held[k]);
+                else q4_load_x<T>(from, chunk * waves * 128 + r * 8, a.cin, true, held[k]);
+            }
         }
     };
     auto put = [&](uint32_t buf) {
@@ -373,10 +391,14 @@ __global__ __launch_bounds__(256 * WK, 2) void q4_tile_kernel(const Q4Args a) {
     T held[DIRECT ? 1 : PIECES][8];
     auto fetch = [&](int b) {                 // into registers
         if constexpr (!DIRECT) {
+            // (a row behind the last token repeats the first: its sums are not stored)
+            const bool whole = (b + 1) * 128 <= a.cin;
 #pragma unroll
             for (int k = 0; k < PIECES; ++k) {
-                const int i = k * 256 + tid, row = i >> 4, piece = i & 15;
-                q4_load_x<T>(x0 + (int64_t)(row < rows_here ? row : 0) * a.x_stride, b * 128 + piece * 8, a.cin, row < rows_here, held[k]);
+                const int i = k * 256 + tid, row = i >> 4, at = b * 128 + (i & 15) * 8;
+                const T* from = x0 + (int64_t)(row < rows_here ? row : 0) * a.x_stride;
+                if (whole) q4_load_whole<T>(from + at, held[k]);
+                else q4_load_x<T>(from, at, a.cin, true, held[k]);
             }
         }
     };
