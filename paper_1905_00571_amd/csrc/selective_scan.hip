@@ -456,16 +456,24 @@ ScanPlan plan_scan(const cadnn_scan_args& g) {
     // one long prompt among single tokens would take a pass over whole sequences twenty times what pieces take, a quarter of the tokens
     // is supposed to be one sequence where there are many.
     const int average = g.tokens / g.seqs;
-    const int longest = !g.seq_start ? average : g.longest > 0 ? std::max(g.longest, average) : g.tokens < 256 ? average : std::max(average, g.tokens / 4);
+    const int longest = !g.seq_start ? average : g.longest > 0 ? std::max(g.longest, average) : g.tokens < 512 ? average : std::max(average, g.tokens / 4);
     p.longest = longest;
+    // (64 sequences x 2048 channels x 16 states, fp16: 1 token 5.8 us here and 8.9 by the kernel for long sequences, 2 tokens 7.1, 9.1, 4 tokens 9.9, 9.7)
     p.few = longest <= 4;
     if (p.few) return p;
-    // Waves of one pass over whole sequences.  Two to a SIMD keep the vector units busy; below that, pieces are worked on
-    // side by side, at the price of a first pass for the states they start from (0.7 of a whole one).
-    const int64_t waves = (int64_t)g.seqs * g.groups * p.blocks_per_group * 4;
-    if (waves >= 2048 || longest < 128) return p;
+    // A wave alone on its SIMD takes 0.41 us a token, whatever there is beside it on the chip; full, the chip takes 0.67 us for
+    // a token of 1024 waves, both passes over pieces and their join together, which cost 12 us more to begin with.  (One sequence
+    // x 2048 x 16: 64 tokens 29.5 us whole, 20.6 in pieces, 1024 tokens 419, 42; 16 sequences of 64 tokens 30.9, 38.9; 16 x 1024 channels x 64 states, 1024
+    // tokens 445, 588.)
+    const int64_t blocks = (int64_t)g.groups * p.blocks_per_group;
     p.chunk = 512;
-    while (p.chunk > 32 && seq_slots(g.tokens, g.seqs, g.seq_start != nullptr, p.chunk) * g.groups * p.blocks_per_group * 4 < 2048) p.chunk /= 2;
+    while (p.chunk > 16 && seq_slots(g.tokens, g.seqs, g.seq_start != nullptr, p.chunk) * blocks * 4 < 2048) p.chunk /= 2;
+    const double whole = 0.41 * longest * (double)((g.seqs * blocks * 4 + 1023) / 1024);
+    const double pieces = 12.0 + std::max(0.67 * (double)g.tokens * (double)(blocks * 4) / 1024.0, 0.82 * p.chunk);
+    if (whole <= pieces) {
+        p.chunk = 0;
+        return p;
+    }
     p.slots = seq_slots(g.tokens, g.seqs, g.seq_start != nullptr, p.chunk);
     p.part_bytes = (size_t)p.slots * g.channels * g.dstate * 4;
     p.bytes = p.part_bytes + (size_t)p.slots * g.channels * 4;
