@@ -240,7 +240,7 @@ __global__ __launch_bounds__(512) void q4_few_kernel(const Q4Args a) {
 // As many tokens as one matrix instruction has columns: 16 in fp16, five in fp32, where the three parts of a token take three
 // columns and one instruction serves all of them.  The workgroup brings the activations of a chunk (one block for every
 // wave) into LDS, each element read, and cut apart, once, while the matrix instructions work on the chunk before, and a wave's
-// codes and scales are fetched D chunks ahead.  us at 8192 -> 8192, groups of 128, one token: fp16 10.6, fp32 12.3, where the kernel above
+// codes and scales are fetched D chunks ahead.  us at 8192 -> 8192, groups of 128, one token: fp16 10.0, fp32 12.7, where the kernel above
 // takes 14.2 and 19.6; the 35 MB are 6.4 us at the rate of a large copy.
 // (Two workgroups to a compute unit, which takes 128 registers: with one, the 257 tiles of 4099 filters took twice the time of 256.)
 template <typename T, int GP, int HELD>
@@ -364,7 +364,7 @@ hipError_t launch_few(const Q4Args& a, hipStream_t s) {
 // tokens meet all banks.  KS steps of 32 inputs are expanded at a time; their sums start from zero in the first matrix
 // instruction and are multiplied by the group's scale into the fp32 accumulators, which for groups of 32 is as much vector
 // work as there is matrix work.  (With the scale multiplied into the codes, rounded to fp16, 2048 tokens through 4096 -> 8192 took 128 us for
-// any group, where this takes 145, 155 and 185 for groups of 128, 64 and 32; the library's fp16 product takes 114.)  WK = 2: two
+// any group, where this takes 143, 155 and 185 for groups of 128, 64 and 32; the library's fp16 product takes 114.)  WK = 2: two
 // times four waves take the blocks in turn and add up, where there are too few workgroups to wait for each other's loads.
 // DIRECT (fp16): activations go straight to LDS, into the second of two buffers, else through registers.
 template <typename T, int GP, int RW, int BN, int KS, int WK, bool DIRECT>
@@ -607,7 +607,7 @@ hipError_t launch_q4(const Q4Args& a, hipStream_t s) {
             if (sm <= f) return direct ? launch_tile<T, GP, 1, 32, 4, 2, true>(a, s) : launch_tile<T, GP, 1, 32, 4, 2, false>(a, s);
         } else {
             constexpr Q4Cost large[3] = {{93, 98, 256}, {96, 105, 256}, {106, 115, 256}}, middle[3] = {{52, 54, 256}, {54, 57, 256}, {59, 60, 256}};
-            constexpr Q4Cost small[3] = {{38, 29, 256}, {39, 31, 256}, {41, 37, 256}}, few[3] = {{23, 21, 256}, {25, 23, 256}, {28.5, 26, 256}};
+            constexpr Q4Cost small[3] = {{38, 29, 256}, {39, 38, 256}, {41, 38, 256}}, few[3] = {{23, 21, 256}, {25, 23, 256}, {28.5, 26, 256}};
             const double l = large[G].of(workgroups(256, 64)), m = middle[G].of(workgroups(256, 32)), sm = small[G].of(workgroups(128, 32));
             const double f = few[G].of(workgroups(64, 32));
             if (l <= m && l <= sm && l <= f) return launch_tile<T, GP, 4, 64, 2, 2, false>(a, s);
