@@ -5,7 +5,8 @@
 // where x~ before a sequence's first token is its tail, the last K - 1 rows that earlier calls saw.  The layer moves every
 // element once and does K multiply-adds with it: memory bounds it, and the launch itself for single tokens.  A thread owns
 // 16 bytes of a row (its channels' taps stay in registers) and a run of tokens, over which it slides a window of rows, four
-// rows loaded at a time; K - 1 rows of a run are read twice.
+// rows loaded at a time; K - 1 rows of a run are read twice.  8192 x 4096, K = 4, SiLU: fp16 33 us, 4.1 TB/s, fp32 48 us, 5.6 TB/s
+// (a large copy: 5.5); element by element, where rows are not 16-byte aligned, fp16 37 us.
 #include <type_traits>
 
 #include "q4.h"
@@ -131,7 +132,7 @@ hipError_t launch_cc_taps(CcArgs a, int taps, hipStream_t s) {
     a.tx_log = 0;
     while (a.tx_log < 8 && (1 << a.tx_log) < vectors) ++a.tx_log;
     // The longest run that still leaves 131072 threads (eight waves to a compute unit): a run of 64 tokens reads 5 % of
-    // the rows twice at K = 4, one of 8 tokens 38 %.
+    // the rows twice at K = 4, one of 8 tokens 38 %.  (8192 x 4096, fp16: 131072 threads 37.4 us, twice as many 40.0.)
     a.chunk = 64;
     while (a.chunk > 8 && seq_slots(a.q.tokens, a.q.seqs, a.q.start != nullptr, a.chunk) * vectors < 131072) a.chunk /= 2;
     a.slots = seq_slots(a.q.tokens, a.q.seqs, a.q.start != nullptr, a.chunk);
