@@ -28,10 +28,10 @@ struct Q4Args {
     const float* bias;
     int64_t x_stride, y_stride;
     int n, cin, cout, blocks, act;
-    int y_vec;      // rows of y are aligned for stores of four elements
 };
 
-// Eight codes of one lane as the left operand of a matrix instruction.
+// Eight codes of one lane as the right operand of a matrix instruction (the left one are activations, so that a lane's four sums
+// are four tokens of one filter, which has one scale).
 template <typename T> struct Q4Frag;
 template <> struct Q4Frag<_Float16> {
     static constexpr int kParts = 1;
@@ -52,7 +52,7 @@ template <> struct Q4Frag<_Float16> {
 #pragma unroll
         for (int e = 0; e < 8; ++e) out[0][e] = v[e];
     }
-    static __device__ __forceinline__ q4_f4 mul(V a, V b, q4_f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ q4_f4 mul(V codes, V x, q4_f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, codes, c, 0, 0, 0); }
 };
 template <> struct Q4Frag<float> {
     static constexpr int kParts = 3;
@@ -91,15 +91,17 @@ template <> struct Q4Frag<float> {
 #pragma unroll
         for (int k = 0; k < 3; ++k) out[k] = p[k].v8;
     }
-    static __device__ __forceinline__ q4_f4 mul(V a, V b, q4_f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ q4_f4 mul(V codes, V x, q4_f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, codes, c, 0, 0, 0); }
 };
 
-// Four scales of a lane's filters.
-__device__ __forceinline__ q4_f4 q4_scales(const _Float16* p) {
-    const q4_h4 v = *(const q4_h4*)p;
-    return (q4_f4){(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
-}
-__device__ __forceinline__ q4_f4 q4_scales(const float* p) { return *(const q4_f4*)p; }
+// The scales of a lane's filter for the groups of a block, as they are stored.
+template <typename T, int GP>
+struct Q4Scales {
+    typedef T V __attribute__((ext_vector_type(GP)));
+    V v;
+    __device__ __forceinline__ void load(const T* at) { v = *(const V*)at; }
+    __device__ __forceinline__ float operator[](int g) const { return (float)v[g]; }
+};
 
 // Eight activations from input i0 on; what lies behind the row's end, or in no row, is zero.  (Rows need not start at
 // multiples of 16 bytes: the loads are as wide for any alignment.)
@@ -134,17 +136,11 @@ __device__ __forceinline__ void q4_load_whole(const T* at, T (&v)[8]) {
     }
 }
 
-// The end of a tile: four filters of one token.
+// The end of a tile: four tokens of one filter.
 template <typename T>
-__device__ __forceinline__ void q4_store(const Q4Args& a, int token, int o0, q4_f4 v) {
-    if (token >= a.n || o0 >= a.cout) return;
-    T* out = (T*)a.y + (int64_t)token * a.y_stride + o0;
-    const bool four = o0 + 4 <= a.cout;
-    if (a.bias) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (four || o0 + e < a.cout) v[e] += a.bias[o0 + e];
-    }
+__device__ __forceinline__ void q4_store(const Q4Args& a, int token, int filter, q4_f4 v) {
+    if (filter >= a.cout) return;
+    if (a.bias) v += a.bias[filter];
     if (a.act == CADNN_ACT_RELU) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = apply_act(v[e], CADNN_ACT_RELU);
@@ -152,14 +148,10 @@ __device__ __forceinline__ void q4_store(const Q4Args& a, int token, int o0, q4_
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = apply_act(v[e], CADNN_ACT_SILU);
     }
-    if (a.y_vec && four) {
-        typedef T V __attribute__((ext_vector_type(4)));
-        *(V*)out = (V){(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
-    } else {
+    T* out = (T*)a.y + (int64_t)token * a.y_stride + filter;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (o0 + e < a.cout) out[e] = (T)v[e];
-    }
+    for (int e = 0; e < 4; ++e)
+        if (token + e < a.n) out[e * a.y_stride] = (T)v[e];
 }
 
 // Few tokens: the weights are read once and bound the kernel.  A workgroup owns 16 * RT filters and 16 * NT tokens and its
@@ -188,13 +180,12 @@ __global__ __launch_bounds__(512) void q4_few_kernel(const Q4Args a) {
     }
     for (int b = wave; b < a.blocks; b += waves) {
         q4_u4 w[RT];
-        q4_f4 sc[RT][GP];
+        Q4Scales<T, GP> sc[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             const int tile = min(tile0 + r, tiles - 1);
             w[r] = *(const q4_u4*)(a.codes + ((int64_t)tile * a.blocks + b) * 256 + lane * 4);
-#pragma unroll
-            for (int p = 0; p < GP; ++p) sc[r][p] = q4_scales((const T*)a.scales + (((int64_t)tile * a.blocks + b) * GP + p) * 16 + 4 * g);
+            sc[r].load((const T*)a.scales + (((int64_t)tile * a.blocks + b) * 16 + j) * GP);
         }
         typename F::V xf[NT][4][F::kParts];
 #pragma unroll
@@ -218,7 +209,7 @@ __global__ __launch_bounds__(512) void q4_few_kernel(const Q4Args a) {
                     for (int p = F::kParts - 1; p >= 0; --p) sum[t] = F::mul(c, xf[t][s][p], sum[t]);
                     if ((s + 1) % (4 / GP) == 0) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[r][t][e] = fmaf(sc[r][s / (4 / GP)][e], sum[t][e], acc[r][t][e]);
+                        for (int e = 0; e < 4; ++e) acc[r][t][e] = fmaf(sc[r][s / (4 / GP)], sum[t][e], acc[r][t][e]);
                     }
                 }
             }
@@ -233,22 +224,22 @@ __global__ __launch_bounds__(512) void q4_few_kernel(const Q4Args a) {
     for (int i = wave; i < RT * NT; i += waves) {
         q4_f4 v = part[i * 64 + lane];
         for (int k = 1; k < waves; ++k) v += part[(k * RT * NT + i) * 64 + lane];
-        q4_store<T>(a, token0 + 16 * (i % NT) + j, (tile0 + i / NT) * 16 + 4 * g, v);
+        q4_store<T>(a, token0 + 16 * (i % NT) + 4 * g, (tile0 + i / NT) * 16 + j, v);
     }
 }
 
 // As many tokens as one matrix instruction has columns: 16 in fp16, five in fp32, where the three parts of a token take three
 // columns and one instruction serves all of them.  The workgroup brings the activations of a chunk (one block for every
 // wave) into LDS, each element read, and cut apart, once, while the matrix instructions work on the chunk before, and a wave's
-// codes and scales are fetched D chunks ahead.  us at 8192 -> 8192, groups of 128, one token: fp16 10.0, fp32 12.7, where the kernel above
-// takes 14.2 and 19.6; the 35 MB are 6.4 us at the rate of a large copy.
+// codes and scales are fetched D chunks ahead.  us at 8192 -> 8192, groups of 128, one token: fp16 9.6, fp32 12.4, where the kernel above
+// takes 14.0 and 19.7; the 35 MB are 6.4 us at the rate of a large copy.
 // (Two workgroups to a compute unit, which takes 128 registers: with one, the 257 tiles of 4099 filters took twice the time of 256.)
 template <typename T, int GP, int HELD>
-__global__ __launch_bounds__(512, sizeof(T) == 4 && GP == 4 && HELD > 1 ? 2 : 4) void q4_columns_kernel(const Q4Args a) {
+__global__ __launch_bounds__(512, 4) void q4_columns_kernel(const Q4Args a) {
     typedef Q4Frag<T> F;
     constexpr int P = F::kParts;
-    constexpr int D = GP == 4 ? 2 : 4;
-    typedef T S4 __attribute__((ext_vector_type(4)));
+    constexpr int D = 4;
+
     extern __shared__ __attribute__((aligned(16))) char q4_smem[];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = (int)blockDim.x >> 6;
     const int j = lane & 15, g = lane >> 4;
@@ -285,15 +276,14 @@ __global__ __launch_bounds__(512, sizeof(T) == 4 && GP == 4 && HELD > 1 ? 2 : 4)
         }
     };
     q4_u4 w[D];
-    S4 sc[D][GP];
+    Q4Scales<T, GP> sc[D];
     q4_f4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
     const uint32_t* const code_at = a.codes + (int64_t)tile * a.blocks * 256 + lane * 4;
-    const T* const scale_at = (const T*)a.scales + (int64_t)tile * a.blocks * (GP * 16) + 4 * g;
+    const T* const scale_at = (const T*)a.scales + (int64_t)tile * a.blocks * (GP * 16) + j * GP;
     auto codes = [&](int slot, int chunk) {
         const int b = min(chunk * waves + wave, a.blocks - 1);      // (behind the last block the activations are zero)
         w[slot] = *(const q4_u4*)(code_at + (int64_t)b * 256);
-#pragma unroll
-        for (int p = 0; p < GP; ++p) sc[slot][p] = *(const S4*)(scale_at + ((int64_t)b * GP + p) * 16);
+        sc[slot].load(scale_at + (int64_t)b * (GP * 16));
     };
 #pragma unroll
     for (int d = 0; d < D; ++d) codes(d, d);
@@ -315,7 +305,7 @@ __global__ __launch_bounds__(512, sizeof(T) == 4 && GP == 4 && HELD > 1 ? 2 : 4)
                     sum = F::mul(F::codes(w[d][s]), xf, s % (4 / GP) == 0 ? (q4_f4){0.0f, 0.0f, 0.0f, 0.0f} : sum);
                     if ((s + 1) % (4 / GP) == 0) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[e] = fmaf((float)sc[d][s / (4 / GP)][e], sum[e], acc[e]);
+                        for (int e = 0; e < 4; ++e) acc[e] = fmaf(sc[d][s / (4 / GP)], sum[e], acc[e]);
                     }
                 }
                 codes(d, c + D);
@@ -325,15 +315,20 @@ __global__ __launch_bounds__(512, sizeof(T) == 4 && GP == 4 && HELD > 1 ? 2 : 4)
             }
         }
     }
-    q4_f4* part = (q4_f4*)q4_smem;       // [wave][lane]
-    part[wave * 64 + lane] = acc;
+    // column c of filter f is element c % 4 of lane c / 4 * 16 + f
+    float* part = (float*)q4_smem;       // [wave][lane][4]
+    *(q4_f4*)(part + (wave * 64 + lane) * 4) = acc;
     __syncthreads();
-    for (int i = tid; i < 4 * a.n; i += (int)blockDim.x) {
-        const int gg = i & 3, token = i >> 2;
-        q4_f4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = tid; i < 16 * a.n; i += (int)blockDim.x) {
+        const int f = i & 15, token = i >> 4, filter = tile * 16 + f;
+        if (filter >= a.cout) continue;
+        float v = 0.0f;
         for (int k = 0; k < waves; ++k)
-            for (int p = P - 1; p >= 0; --p) v += part[k * 64 + gg * 16 + token * P + p];
-        q4_store<T>(a, token, tile * 16 + 4 * gg, v);
+            for (int p = P - 1; p >= 0; --p) {
+                const int c = token * P + p;
+                v += part[(k * 64 + (c >> 2) * 16 + f) * 4 + (c & 3)];
+            }
+        ((T*)a.y)[(int64_t)token * a.y_stride + filter] = (T)apply_act(v + (a.bias ? a.bias[filter] : 0.0f), a.act);
     }
 }
 
@@ -364,7 +359,7 @@ hipError_t launch_few(const Q4Args& a, hipStream_t s) {
 // tokens meet all banks.  KS steps of 32 inputs are expanded at a time; their sums start from zero in the first matrix
 // instruction and are multiplied by the group's scale into the fp32 accumulators, which for groups of 32 is as much vector
 // work as there is matrix work.  (With the scale multiplied into the codes, rounded to fp16, 2048 tokens through 4096 -> 8192 took 128 us for
-// any group, where this takes 143, 155 and 185 for groups of 128, 64 and 32; the library's fp16 product takes 114.)  WK = 2: two
+// any group, where this takes 143, 153 and 180 for groups of 128, 64 and 32; the library's fp16 product takes 114.)  WK = 2: two
 // times four waves take the blocks in turn and add up, where there are too few workgroups to wait for each other's loads.
 // DIRECT (fp16): activations go straight to LDS, into the second of two buffers, else through registers.
 template <typename T, int GP, int RW, int BN, int KS, int WK, bool DIRECT>
@@ -448,7 +443,7 @@ __global__ __launch_bounds__(256 * WK, 2) void q4_tile_kernel(const Q4Args a) {
     for (int r = 0; r < RW; ++r) {
         const int tile = min(tile0 + r, tiles - 1);
         code_at[r] = a.codes + (int64_t)tile * a.blocks * 256 + lane * 4;
-        scale_at[r] = (const T*)a.scales + (int64_t)tile * a.blocks * GP * 16 + 4 * g;
+        scale_at[r] = (const T*)a.scales + (int64_t)tile * a.blocks * GP * 16 + j * GP;
     }
     const int steps = (a.blocks + WK - 1) / WK;
     q4_u4 w[RW];
@@ -474,14 +469,17 @@ __global__ __launch_bounds__(256 * WK, 2) void q4_tile_kernel(const Q4Args a) {
 #pragma unroll
         for (int r = 0; r < RW; ++r) wn[r] = *(const q4_u4*)(code_at[r] + (int64_t)next * 256);
         if (WK == 1 || b < a.blocks) {
+            Q4Scales<T, GP> scales[RW];
+#pragma unroll
+            for (int r = 0; r < RW; ++r) scales[r].load(scale_at[r] + (int64_t)b * (GP * 16));
 #pragma unroll
             for (int ph = 0; ph < 4 / KS; ++ph) {
-                q4_f4 sc[RW][KS / PER];
+                float sc[RW][KS / PER];
                 typename F::V af[RW][KS];
 #pragma unroll
                 for (int r = 0; r < RW; ++r) {
 #pragma unroll
-                    for (int q = 0; q < KS / PER; ++q) sc[r][q] = q4_scales(scale_at[r] + ((int64_t)b * GP + (ph * KS + q * PER) * GP / 4) * 16);
+                    for (int q = 0; q < KS / PER; ++q) sc[r][q] = scales[r][(ph * KS + q * PER) * GP / 4];
 #pragma unroll
                     for (int s = 0; s < KS; ++s) af[r][s] = F::codes(w[r][ph * KS + s]);
                 }
@@ -505,7 +503,7 @@ __global__ __launch_bounds__(256 * WK, 2) void q4_tile_kernel(const Q4Args a) {
 #pragma unroll
                             for (int r = 0; r < RW; ++r)
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) acc[r][c][e] = fmaf(sc[r][s / PER][e], sum[r][e], acc[r][c][e]);
+                                for (int e = 0; e < 4; ++e) acc[r][c][e] = fmaf(sc[r][s / PER], sum[r][e], acc[r][c][e]);
                         }
                     }
                 }
@@ -540,7 +538,7 @@ __global__ __launch_bounds__(256 * WK, 2) void q4_tile_kernel(const Q4Args a) {
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
-        for (int r = 0; r < RW; ++r) q4_store<T>(a, token0 + c * 16 + j, (tile0 + r) * 16 + 4 * g, acc[r][c]);
+        for (int r = 0; r < RW; ++r) q4_store<T>(a, token0 + c * 16 + 4 * g, (tile0 + r) * 16 + j, acc[r][c]);
 }
 
 // More than 64 KiB of dynamic LDS have to be asked for, once for a kernel on a device.
@@ -607,7 +605,7 @@ hipError_t launch_q4(const Q4Args& a, hipStream_t s) {
             if (sm <= f) return direct ? launch_tile<T, GP, 1, 32, 4, 2, true>(a, s) : launch_tile<T, GP, 1, 32, 4, 2, false>(a, s);
         } else {
             constexpr Q4Cost large[3] = {{93, 98, 256}, {96, 105, 256}, {106, 115, 256}}, middle[3] = {{52, 54, 256}, {54, 57, 256}, {59, 60, 256}};
-            constexpr Q4Cost small[3] = {{38, 29, 256}, {39, 38, 256}, {41, 38, 256}}, few[3] = {{23, 21, 256}, {25, 23, 256}, {28.5, 26, 256}};
+            constexpr Q4Cost small[3] = {{38, 29, 256}, {39, 31, 256}, {41, 38, 256}}, few[3] = {{23, 21, 256}, {25, 23, 256}, {28.5, 26, 256}};
             const double l = large[G].of(workgroups(256, 64)), m = middle[G].of(workgroups(256, 32)), sm = small[G].of(workgroups(128, 32));
             const double f = few[G].of(workgroups(64, 32));
             if (l <= m && l <= sm && l <= f) return launch_tile<T, GP, 4, 64, 2, 2, false>(a, s);
@@ -618,7 +616,7 @@ hipError_t launch_q4(const Q4Args& a, hipStream_t s) {
     }
     // Staged activations pay from rows of some length on (one token, 512 -> 512: fp16 3.5 staged, 2.9 not; 4096 -> 4096: 5.0, 5.9).
     if (a.n <= 16 / Q4Frag<T>::kParts && a.blocks > (sizeof(T) == 2 ? 16 : 8)) return launch_columns<T, GP>(a, s);
-    // (13 tokens, 5003 -> 4099, fp16: one tile of filters a wave 24.6, two 15.8; 4096 filters 14.6, 15.9)
+    // (13 tokens, 5003 -> 4099, groups of 32, fp16: one tile of filters a wave 22.5, two 14.5; 4096 filters, one 14.6, two 15.9)
     if (a.n <= 16) return a.cout > 16 * 256 && a.blocks > 8 ? launch_few<T, GP, 2, 1>(a, s) : launch_few<T, GP, 1, 1>(a, s);
     constexpr bool h = sizeof(T) == 2;
     constexpr Q4Cost few1 = {h ? 7.3 : 11.3, h ? 12.5 : 20, 512}, few2 = {h ? 9.3 : 11.8, h ? 13 : 21.5, 512}, few4 = {h ? 11.5 : 15.2, h ? 17.0 : 29, 512};
@@ -644,7 +642,6 @@ cadnn_status launch_q4_fc(const cadnn_q4_weights* w, const void* x, int64_t x_st
         a.x = (const char*)x + (size_t)n0 * x_stride * e; a.y = (char*)y + (size_t)n0 * y_stride * e;
         a.x_stride = x_stride; a.y_stride = y_stride;
         a.n = std::min(step, n - n0); a.cin = w->cin; a.cout = w->cout; a.blocks = (w->cin + kQ4Block - 1) / kQ4Block; a.act = act;
-        a.y_vec = (uintptr_t)a.y % (4 * e) == 0 && y_stride % 4 == 0;
         CADNN_HIP(w->dtype == CADNN_F16 ? launch_q4_group<_Float16>(a, w->group, s) : launch_q4_group<float>(a, w->group, s));
     }
     return CADNN_OK;

@@ -46,10 +46,10 @@ inline int get_code(const uint8_t* row, int i) { return ((row[i >> 1] >> ((i & 1
 
 // Device layout.  Filters come in tiles of 16, inputs in blocks of 128; a tile's blocks follow each other, 1024 bytes each:
 // lane l of a wave owns the 16 bytes at 16 * l, filter l % 16 and, in dword s (a step of 32 inputs), the eight inputs
-// 32 * s + 8 * (l / 16) onwards -- what one lane of a 16 x 16 x 32 matrix instruction holds of its left operand, so that
+// 32 * s + 8 * (l / 16) onwards -- what one lane of a 16 x 16 x 32 matrix instruction holds of an operand, so that
 // a wave reads whole kilobytes and moves nothing between lanes.  In a dword nibble t holds element 2t and nibble 4 + t
 // element 2t + 1: a shift and a mask leave two neighbours in the two halves of the register.  Scales lie as
-// [tile][group][16 filters].  What lies behind the last filter or input has code 0 (8 as stored) and scale 0.
+// [tile][block][16 filters][groups of the block]: one load for a lane, whose sums are all of one filter.  What lies behind the last filter or input has code 0 (8 as stored) and scale 0.
 cadnn_status ensure_q4_device(const cadnn_q4_weights* w, const char* who, hipStream_t stream, bool has_stream) {
     std::lock_guard<std::mutex> lock(w->mu);
     int device = -1;
@@ -100,7 +100,7 @@ cadnn_status ensure_q4_device(const cadnn_q4_weights* w, const char* who, hipStr
         else f.assign(padded, 0.0f);
         for (int o = 0; o < w->cout; ++o)
             for (int g = 0; g < w->groups; ++g) {
-                const size_t at = ((size_t)(o / kQ4Rows) * blocks * per + g) * kQ4Rows + o % kQ4Rows;
+                const size_t at = (((size_t)(o / kQ4Rows) * blocks + g / per) * kQ4Rows + o % kQ4Rows) * per + g % per;
                 const float s = w->scales[(size_t)o * w->groups + g];
                 if (w->dtype == CADNN_F16) h[at] = f32_to_f16_rne(s);
                 else f[at] = 16.0f * s;      // (the kernels' fp32 codes are sixteenths)
