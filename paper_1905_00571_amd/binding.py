@@ -589,9 +589,11 @@ def cadnn_selective_scan(x, dt, a, b, c, d=None, z=None, dt_bias=None, softplus:
     g = _scan_args(x, dt, a, b, c, d, z, dt_bias, softplus, state, seq_start, seqs, longest, out)
     L, ref = lib(), ctypes.byref(g)
     if workspace is None:
-        nbytes = ctypes.c_size_t()
-        _check(L.cadnn_selective_scan_workspace_bytes(ref, ctypes.byref(nbytes)))
-        size = nbytes.value
+        size = 0
+        if x.shape[0] > seqs:          # (single tokens need none: the question is not worth its microsecond)
+            nbytes = ctypes.c_size_t()
+            _check(L.cadnn_selective_scan_workspace_bytes(ref, ctypes.byref(nbytes)))
+            size = nbytes.value
         if size:
             import torch
             workspace = torch.empty(size, dtype=torch.uint8, device=x.device)

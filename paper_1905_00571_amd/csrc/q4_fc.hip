@@ -605,13 +605,14 @@ hipError_t launch_q4(const Q4Args& a, hipStream_t s) {
             if (sm <= f) return direct ? launch_tile<T, GP, 1, 32, 4, 2, true>(a, s) : launch_tile<T, GP, 1, 32, 4, 2, false>(a, s);
         } else {
             constexpr Q4Cost large[3] = {{93, 98, 256}, {96, 105, 256}, {106, 115, 256}}, middle[3] = {{52, 54, 256}, {54, 57, 256}, {59, 60, 256}};
-            constexpr Q4Cost small[3] = {{38, 29, 256}, {39, 31, 256}, {41, 38, 256}}, few[3] = {{23, 21, 256}, {25, 23, 256}, {28.5, 26, 256}};
+            constexpr Q4Cost small[3] = {{38, 29, 256}, {39, 31, 256}, {41, 38, 256}}, few[3] = {{22.5, 20.5, 256}, {22.5, 20.5, 256}, {23, 21, 256}};
+            constexpr Q4Cost fewer[3] = {{16.5, 25, 512}, {16.5, 29.5, 512}, {17, 29.5, 512}};
             const double l = large[G].of(workgroups(256, 64)), m = middle[G].of(workgroups(256, 32)), sm = small[G].of(workgroups(128, 32));
-            const double f = few[G].of(workgroups(64, 32));
+            const double f2 = few[G].of(workgroups(64, 32)), f1 = fewer[G].of(workgroups(64, 16)), f = std::min(f1, f2);
             if (l <= m && l <= sm && l <= f) return launch_tile<T, GP, 4, 64, 2, 2, false>(a, s);
             if (m <= sm && m <= f) return launch_tile<T, GP, 4, 32, 4, 2, false>(a, s);
             if (sm <= f) return launch_tile<T, GP, 2, 32, 4, 2, false>(a, s);
-            if (workgroups(64, 32) >= 256) return launch_few<T, GP, 4, 2>(a, s);
+            if (f2 <= f1 && workgroups(64, 32) >= 256) return launch_few<T, GP, 4, 2>(a, s);
         }
     }
     // Staged activations pay from rows of some length on (one token, 512 -> 512: fp16 3.5 staged, 2.9 not; 4096 -> 4096: 5.0, 5.9).
@@ -619,7 +620,7 @@ hipError_t launch_q4(const Q4Args& a, hipStream_t s) {
     // (13 tokens, 5003 -> 4099, groups of 32, fp16: one tile of filters a wave 22.5, two 14.5; 4096 filters, one 14.6, two 15.9)
     if (a.n <= 16) return a.cout > 16 * 256 && a.blocks > 8 ? launch_few<T, GP, 2, 1>(a, s) : launch_few<T, GP, 1, 1>(a, s);
     constexpr bool h = sizeof(T) == 2;
-    constexpr Q4Cost few1 = {h ? 7.3 : 11.3, h ? 12.5 : 20, 512}, few2 = {h ? 9.3 : 11.8, h ? 13 : 21.5, 512}, few4 = {h ? 11.5 : 15.2, h ? 17.0 : 29, 512};
+    constexpr Q4Cost few1 = {h ? 7.3 : 11.3, h ? 12.5 : 20, 512}, few2 = {h ? 9.3 : 11.8, h ? 13 : 21.5, 512}, few4 = {h ? 11.5 : 16.5, h ? 16.5 : 27, 512};
     const double f1 = few1.of(workgroups(16, 16)), f2 = few2.of(workgroups(32, 16)), f4 = few4.of(workgroups(64, 16));
     return f4 <= f2 && f4 <= f1 ? launch_few<T, GP, 4, 1>(a, s) : f2 <= f1 ? launch_few<T, GP, 2, 1>(a, s) : launch_few<T, GP, 1, 1>(a, s);
 }
