@@ -177,7 +177,7 @@ cadnn_status cadnn_fc_prepare(const cadnn_weights* w);
  * magnitude / 7.  cadnn_q4_pack_codes takes HOST codes [cout][cin] and scales [cout][groups] that
  * some quantisation has made.  For CADNN_F16 the scales are rounded to the nearest binary16 (before the
  * codes are chosen).  Packing is pure host work; the device layout is uploaded by the first call, to the
- * device that is current then, or by cadnn_q4_prepare; the handle stays on that device.
+ * device that is current then, or by cadnn_q4_prepare; the handle stays on that device and outlives the nets and graphs that use it.
  * Errors: EINVAL (NULL pointer, non-positive size, unknown dtype, a code outside -8..7, a weight or scale
  * that is not finite or of 2^120 and more, or beyond binary16 for CADNN_F16); EUNSUPPORTED (group other than
  * 32, 64, 128; cin or cout above 2^24); ENOMEM.  *out is set to NULL on failure.
@@ -240,7 +240,7 @@ cadnn_status cadnn_causal_conv1d(const cadnn_weights* w, const void* x, int64_t 
  * a: fp32 [channels][dstate]; d, dt_bias: fp32 [channels] or NULL (0); z: NULL for no gate.  state: fp32
  * [seqs][channels][dstate] or NULL.  Sums and states are fp32.  y must not overlap what is read.  All of it in
  * memory of the current device.
- * workspace: device memory of cadnn_selective_scan_workspace_bytes bytes (0 for many calls), used by this call alone until it is through: long
+ * workspace: device memory of cadnn_selective_scan_workspace_bytes bytes (0 for many calls, and always for single tokens), used by this call alone until it is through: long
  * sequences that are too few to fill the chip are cut into pieces that run side by side.  Without it, or with
  * less, every sequence is worked on from end to end: slower, and with differently rounded sums.
  * Errors: EINVAL (NULL pointer, bad sizes or strides as above, channels that are no multiple of groups, a

@@ -258,3 +258,89 @@ def test_q4_fc_refuses_tensors_that_do_not_fit():
     with pytest.raises(cad.CadnnError):
         cad.cadnn_q4_fc(h, x[:0])
     h.free()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_q4_fc_with_negative_and_vanishing_scales(dtype):
+    tt, flag = TYPES[dtype]
+    codes, scales = layer(50, 384, 128, dtype, 21)
+    scales[::2, 1] *= -1
+    scales[3:9] = 0.0
+    scales[11] = 2.0 ** -24 if dtype == "f16" else 2.0 ** -140          # below the normal numbers
+    h = cad.cadnn_q4_pack_codes(codes, scales, 128, flag)
+    x = torch.from_numpy(np.random.default_rng(22).standard_normal((40, 384)).astype(np.float32)).to(tt)
+    for n in (1, 40):
+        y = cad.cadnn_q4_fc(h, x[:n].cuda())
+        ref, mag = reference(codes, scales, 128, x[:n].float().numpy(), None, cad.ACT_NONE)
+        rows = [r for r in range(50) if r != 11]
+        check(y[:, rows], ref[:, rows], mag[:, rows], 384, dtype)
+        # (row 11: sums of products below the normal numbers, rounded to their steps at most once a group and once in the end)
+        step = 2.0 ** -24 if dtype == "f16" else 2.0 ** -149
+        assert (np.abs(y[:, 11].double().cpu().numpy() - ref[:, 11]) <= 3 * step + 2.0 ** -10 * np.abs(ref[:, 11])).all()
+    h.free()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,n", [("f16", 1100), ("f32", 600), ("f16", 9), ("f32", 4)])
+def test_q4_fc_rows_far_apart(dtype, n):
+    """Offsets beyond 2^31 elements, in x and in y."""
+    tt, flag = TYPES[dtype]
+    stride = 2 ** 31 // n + 4096 + (1 if n < 16 else 0)
+    codes, scales = layer(130, 256, 64, dtype, 23)
+    h = cad.cadnn_q4_pack_codes(codes, scales, 64, flag)
+    values = torch.from_numpy(np.random.default_rng(24).standard_normal((n, 256)).astype(np.float32)).to(tt)
+    x = torch.empty_strided((n, 256), (stride, 1), dtype=tt, device="cuda")
+    out = torch.empty_strided((n, 130), (stride, 1), dtype=tt, device="cuda")
+    x.copy_(values)
+    cad.cadnn_q4_fc(h, x, out=out)
+    ref, mag = reference(codes, scales, 64, values.float().numpy(), None, cad.ACT_NONE)
+    check(out, ref, mag, 256, dtype)
+    h.free()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,cin,cout", [(1500, 300, 2100), (2000, 512, 1024)])
+def test_q4_fc_first_call_of_a_kernel_in_a_graph(n, cin, cout):
+    """Prepared weights are enough for a call to be captured, whatever its kernel asks of the device."""
+    codes, scales = layer(cout, cin, 32, "f32", 25)
+    h = cad.cadnn_q4_pack_codes(codes, scales, 32, cad.F32)
+    cad.cadnn_q4_prepare(h)
+    x = torch.randn(n, cin, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = cad.cadnn_q4_fc(h, x, None, cad.ACT_SILU)
+    for k in range(3):
+        x.copy_(torch.randn(n, cin, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, cad.cadnn_q4_fc(h, x, None, cad.ACT_SILU))
+    ref, mag = reference(codes, scales, 32, x.cpu().numpy(), None, cad.ACT_SILU)
+    check(y, ref, mag, cin, "f32")
+    h.free()
+
+
+@pytest.mark.gpu
+def test_q4_fc_from_two_threads_at_once():
+    """The first calls on a handle, side by side: one of them uploads the weights, both use them."""
+    import threading
+    codes, scales = layer(600, 1024, 64, "f16", 26)
+    x = torch.randn(20, 1024, device="cuda").half()
+    for _ in range(3):
+        h = cad.cadnn_q4_pack_codes(codes, scales, 64, cad.F16)
+        torch.cuda.synchronize()
+        got = [None, None]
+
+        def work(i):
+            s = torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                got[i] = cad.cadnn_q4_fc(h, x)
+            s.synchronize()
+
+        threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        assert torch.equal(got[0], got[1]) and torch.equal(got[0], cad.cadnn_q4_fc(h, x))
+        h.free()

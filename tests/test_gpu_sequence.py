@@ -213,7 +213,8 @@ def test_selective_scan(dtype, lens, channels, dstate, groups):
     starts = starts_of(lens)
     what = f"{lens}, {channels} channels, {dstate} states, {groups} groups"
     ref, bound, last, off = scan_reference(v, starts, True, True)
-    runs = [{"seq_start": dev(starts)}, {"seq_start": dev(starts), "longest": max(lens)}, {"seq_start": dev(starts), "longest": 1}, {"seq_start": dev(starts), "workspace": torch.empty(0, dtype=torch.uint8, device="cuda")}]
+    runs = [{"seq_start": dev(starts)}, {"seq_start": dev(starts), "longest": max(lens)}, {"seq_start": dev(starts), "longest": 1}, {"seq_start": dev(starts), "workspace": torch.empty(0, dtype=torch.uint8, device="cuda")},
+            {"seq_start": dev(starts), "workspace": torch.empty(64, dtype=torch.uint8, device="cuda")}]
     if len(set(lens)) == 1:
         runs.append({"seq_start": None})
     for how in runs:
@@ -313,6 +314,59 @@ def test_selective_scan_with_masked_steps_and_values_that_are_not_finite(tokens,
     others = [c for c in range(70) if c != 7]
     check(y[:, others], ref[:, others], bound[:, others], "f32")
     check(kept[:, others], last[:, others], off[:, others], "f32")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [12, 400, 3000])
+def test_selective_scan_cuts_bad_offsets(tokens):
+    """Offsets that lie outside the rows or descend change no row and no state but those of the call's own tensors."""
+    channels, n = 40, 16
+    v = scan_inputs([tokens], channels, n, 1, np.float32, 9)
+    t = {k: dev(a) for k, a in v.items()}
+    out = torch.full((tokens + 20, channels), 7.0, device="cuda")
+    states = torch.full((5, channels, n), 3.0, device="cuda")
+    for starts in ([-9, tokens, tokens // 3, 10 ** 6], [0, -1, -2, -3], [10 ** 9, 10 ** 9, 5, 9], [tokens, 0, tokens, 0]):
+        cad.cadnn_selective_scan(t["x"], t["dt"], t["a"], t["b"], t["c"], softplus=True, state=states[1:4], seqs=3, out=out[10:10 + tokens],
+                                 seq_start=torch.tensor(starts, dtype=torch.int32, device="cuda"))
+        torch.cuda.synchronize()
+    assert bool((out[:10] == 7.0).all()) and bool((out[10 + tokens:] == 7.0).all())
+    assert bool((states[0] == 3.0).all()) and bool((states[4] == 3.0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("tokens,seqs", [(900, 1), (900, 300)])
+def test_rows_far_apart(dtype, tokens, seqs):
+    """Offsets beyond 2^31 elements, in all tensors that have rows."""
+    tt, flag, npt = TYPES[dtype]
+    channels, n = 24, 16
+    stride = 2 ** 31 // tokens + 4096
+    lens = [tokens // seqs] * seqs
+    starts = starts_of(lens)
+    v = scan_inputs(lens, channels, n, 1, npt, 10)
+
+    def far(a):
+        a = dev(a.reshape(tokens, -1))
+        w = torch.empty_strided(a.shape, (stride, 1), dtype=a.dtype, device="cuda")
+        return w.copy_(a)
+
+    t = {k: far(a) if k in ("x", "dt", "z", "b", "c") else dev(a) for k, a in v.items()}
+    out = torch.empty_strided((tokens, channels), (stride, 1), dtype=tt, device="cuda")
+    cad.cadnn_selective_scan(t["x"], t["dt"], t["a"], t["b"], t["c"], d=t["d"], z=t["z"], dt_bias=t["dt_bias"], softplus=True, state=t["state"],
+                             seqs=seqs, out=out)
+    ref, bound, last, off = scan_reference(v, starts, True, True)
+    check(out, ref, bound, dtype)
+    check(t["state"], last, off, "f32")
+    g = np.random.default_rng(11)
+    w = g.uniform(-1, 1, (channels, 4)).astype(npt).astype(np.float32)
+    state = g.standard_normal((seqs, 3, channels)).astype(npt)
+    h = cad.cadnn_pack_weights(w.reshape(channels, 1, 1, 4), flag)
+    kept = dev(state)
+    cad.cadnn_causal_conv1d(h, t["x"], kept, None, seqs, None, cad.ACT_SILU, out=out)
+    ref, bound, last = conv_reference(v["x"], w, None, state, starts, cad.ACT_SILU)
+    check(out, ref, bound, dtype)
+    assert np.array_equal(kept.double().cpu().numpy(), last)
+    h.free()
 
 
 # ---- together ---------------------------------------------------------------------------------------
