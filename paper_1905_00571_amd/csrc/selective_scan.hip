@@ -8,7 +8,7 @@
 // SIMD per 64 of them, against 4 / N elements of traffic: from N = 16 on the vector units bound a long scan, and the
 // states' traffic a single token.  A long sequence is a chain of tokens that only channels and states run beside, so it is cut into
 // pieces: one pass for what each piece ends with, a join, one for the outputs -- the exponentials are taken twice.  us at 4096
-// tokens x 2048 channels x 16 states, gated, fp16: 37 + 10 + 48 (two waves a SIMD; 20 for the vector work of one pass at its rate, 12 for the
+// tokens x 2048 channels x 16 states, gated, fp16: 38 + 7 + 49 (two waves a SIMD; 20 for the vector work of one pass at its rate, 12 for the
 // traffic); one token of 64 sequences x 4096 x 16: 11.8, 3.1 TB/s.
 #include <type_traits>
 
@@ -65,6 +65,23 @@ __device__ __forceinline__ float ss_sum(float v) {
     return v;
 }
 
+// f of eight values that four neighbouring lanes all hold: lane q takes values q and 4 + q, and passes them on.
+// (softplus and silu of steps and gates took a tenth of the time where four lanes of a channel each worked out all of them: 1501 tokens x 1000
+// channels x 64 states, fp32, passes 37.3 + 45.0 us, so 34.0 + 40.1)
+template <typename F>
+__device__ __forceinline__ void ss_shared(float (&v)[8], int sub, F f) {
+    const int q = sub & 3;
+#pragma unroll
+    for (int k = 0; k < 8; k += 4) {
+        const float own = f(q == 0 ? v[k] : q == 1 ? v[k + 1] : q == 2 ? v[k + 2] : v[k + 3]);
+        const int bits = (int)__float_as_uint(own);
+        v[k] = __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp(bits, 0x00, 0xf, 0xf, true));
+        v[k + 1] = __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp(bits, 0x55, 0xf, 0xf, true));
+        v[k + 2] = __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp(bits, 0xaa, 0xf, 0xf, true));
+        v[k + 3] = __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp(bits, 0xff, 0xf, 0xf, true));
+    }
+}
+
 // NS consecutive floats of a lane, `left` of which exist; 16 bytes at a time where all do (4-byte alignment is enough).
 template <int NS>
 __device__ __forceinline__ void ss_load(const float* p, int left, float (&v)[NS]) {
@@ -106,6 +123,7 @@ enum ScanPass {
 template <typename T, int NS, int L, int PASS, bool FULL>
 __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
     constexpr int CH = 256 / L, N = NS * L, TT = kScanTile;
+    static_assert(TT == 8, "ss_shared");
     constexpr int ROW = PASS == SCAN_ENDS ? N : 2 * N;          // elements of a token in LDS
     constexpr int PER = (TT * ROW + 255) / 256;                 // of them fetched by a thread
     constexpr int V = 16 / (int)sizeof(T);
@@ -209,11 +227,21 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
 #pragma unroll
         for (int u = 0; u < TT; ++u) {
             dt[u] += bias;
-            if (a.softplus) dt[u] = ss_softplus(dt[u]);
-            if (PASS == SCAN_ENDS) steps += u < left ? dt[u] : 0.0f;
-            else if (a.z) z[u] = ss_silu(z[u]);
+            if (L < 4) {
+                if (a.softplus) dt[u] = ss_softplus(dt[u]);
+                if (PASS != SCAN_ENDS && a.z) z[u] = ss_silu(z[u]);
+            }
         }
-        span += steps;
+        if constexpr (L >= 4) {
+            // (each of four lanes of a channel works out two tokens' and tells the others)
+            if (a.softplus) ss_shared(dt, sub, [](float v) { return ss_softplus(v); });
+            if (PASS != SCAN_ENDS && a.z) ss_shared(z, sub, [](float v) { return ss_silu(v); });
+        }
+        if (PASS == SCAN_ENDS) {
+#pragma unroll
+            for (int u = 0; u < TT; ++u) steps += u < left ? dt[u] : 0.0f;
+            span += steps;
+        }
         float ys[TT];
         // (outputs are stored behind the tile: a store under a condition would part the tokens' work from each other)
         // one token: three full-rate operations a state beside the exponential and the product under it
@@ -271,7 +299,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
 // Joins the pieces of each sequence, h = exp(a * span) * h + end; what a piece ended with is replaced by what it starts from.
 // A workgroup owns 64 (channel, state) pairs of a sequence.  Its four waves fetch S pieces each, join them from zero, learn
 // from each other what they start from, and go through them again, in registers: the chain of a long sequence costs one
-// round trip to memory for 4 * S pieces.  (One thread for a pair's whole chain took 12.5 us for 64 pieces of 32768 pairs.)
+// round trip to memory for 4 * S pieces.  (64 pieces of 32768 pairs: 12.5 us with one thread for a pair's whole chain, 9.8 with S = 32, 6.6 with S = 16.)
 template <int S>
 __device__ __forceinline__ float ss_join(const SsArgs& a, int64_t per_seq, int64_t i, int ch, int64_t first, int p0, int pieces, float al, float h, float (&lds)[2][4][64]) {
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
@@ -326,7 +354,8 @@ __global__ __launch_bounds__(256) void scan_join_kernel(const SsArgs a) {
     float* kept = a.state ? a.state + (int64_t)s * per_seq + i : nullptr;
     float h = kept ? *kept : 0.0f;
     int p = 0;
-    for (; pieces - p > 32; p += 128) h = ss_join<32>(a, per_seq, i, ch, first, p, pieces, al, h, lds);
+    for (; pieces - p > 64; p += 128) h = ss_join<32>(a, per_seq, i, ch, first, p, pieces, al, h, lds);
+    for (; pieces - p > 32; p += 64) h = ss_join<16>(a, per_seq, i, ch, first, p, pieces, al, h, lds);
     for (; p < pieces; p += 32) h = ss_join<8>(a, per_seq, i, ch, first, p, pieces, al, h, lds);
     if (kept && at < per_seq && threadIdx.x < 64) *kept = h;
 }
