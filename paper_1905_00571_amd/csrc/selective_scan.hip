@@ -8,7 +8,7 @@
 // SIMD per 64 of them, against 4 / N elements of traffic: from N = 16 on the vector units bound a long scan, and the
 // states' traffic a single token.  A long sequence is a chain of tokens that only channels and states run beside, so it is cut into
 // pieces: one pass for what each piece ends with, a join, one for the outputs -- the exponentials are taken twice.  us at 4096
-// tokens x 2048 channels x 16 states, gated, fp16: 38 + 7 + 49 (two waves a SIMD; 20 for the vector work of one pass at its rate, 12 for the
+// tokens x 2048 channels x 16 states, gated, fp16: 36 + 7 + 44 (two waves a SIMD; 20 for the vector work of one pass at its rate, 12 for the
 // traffic); one token of 64 sequences x 4096 x 16: 11.8, 3.1 TB/s.
 #include <type_traits>
 
@@ -37,16 +37,22 @@ struct SsArgs {
 
 __device__ __forceinline__ float ss_exp2(float v) { return __builtin_amdgcn_exp2f(v); }
 
-// log(1 + exp(v)).  exp(v) from the product v * log2(e) in two parts; below 1/16 the series of log1p, whose first term
-// left out is under 2^-26 of the value, and above it log(u) corrected for the rounding of u = 1 + e.
+// log(1 + exp(v)) = max(v, 0) + log1p(e), e = exp(-|v|), from the product |v| * log2(e) in two parts.  log1p(e) = e + e^2 q(e), whose q of
+// degree 8 was fitted to it for 0 <= e <= 1 (relative error 2^-27, 1.4 * 2^-24 with the roundings of its evaluation).
 __device__ __forceinline__ float ss_softplus(float v) {
-    v = v < -150.0f ? -150.0f : v;      // (exp is zero from there on; the two parts of -infinity would be no numbers)
-    const float hi = v * 1.44269502f, lo = fmaf(v, 1.44269502f, -hi) + v * 1.92596303e-8f;
+    const float m = fminf(fabsf(v), 150.0f);      // (exp is zero from there on; the two parts of an infinity would be no numbers)
+    const float hi = m * -1.44269502f, lo = fmaf(m, -1.92596303e-8f, fmaf(m, -1.44269502f, -hi));
     const float e = ss_exp2(hi) * fmaf(lo, 0.693147182f, 1.0f);
-    const float series = e * fmaf(e, fmaf(e, fmaf(e, fmaf(e, fmaf(e, -0.166666672f, 0.2f), -0.25f), 0.333333343f), -0.5f), 1.0f);
-    const float u = 1.0f + e;
-    const float logs = fmaf(__builtin_amdgcn_logf(u), 0.693147182f, (e - (u - 1.0f)) * __builtin_amdgcn_rcpf(u));
-    return v > 20.0f ? v : e < 0.0625f ? series : logs;
+    float q = -0.00324401166f;
+    q = fmaf(q, e, 0.0198514052f);
+    q = fmaf(q, e, -0.0569594353f);
+    q = fmaf(q, e, 0.106036462f);
+    q = fmaf(q, e, -0.153055876f);
+    q = fmaf(q, e, 0.196759388f);
+    q = fmaf(q, e, -0.249541342f);
+    q = fmaf(q, e, 0.333299637f);
+    q = fmaf(q, e, -0.499999017f);
+    return (v < 0.0f ? 0.0f : v) + fmaf(q * e, e, e);      // (no number stays none)
 }
 
 __device__ __forceinline__ float ss_silu(float v) {
@@ -67,7 +73,7 @@ __device__ __forceinline__ float ss_sum(float v) {
 
 // f of eight values that four neighbouring lanes all hold: lane q takes values q and 4 + q, and passes them on.
 // (softplus and silu of steps and gates took a tenth of the time where four lanes of a channel each worked out all of them: 1501 tokens x 1000
-// channels x 64 states, fp32, passes 37.3 + 45.0 us, so 34.0 + 40.1)
+// channels x 64 states, fp32, passes 37.3 + 45.0 us, so 34.0 + 40.1; with log1p as a polynomial and one branch a tile 33.7 + 38.1)
 template <typename F>
 __device__ __forceinline__ void ss_shared(float (&v)[8], int sub, F f) {
     const int q = sub & 3;
@@ -168,7 +174,10 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
                 nd[u] = *(const T*)(d + lane_at);
                 x += a.x_stride * (int64_t)sizeof(T);
                 d += a.dt_stride * (int64_t)sizeof(T);
-                if (PASS != SCAN_ENDS && z) {
+            }
+            if (PASS != SCAN_ENDS && z) {
+#pragma unroll
+                for (int u = 0; u < TT; ++u) {
                     nz[u] = *(const T*)(z + lane_at);
                     z += a.z_stride * (int64_t)sizeof(T);
                 }
@@ -227,15 +236,21 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
 #pragma unroll
         for (int u = 0; u < TT; ++u) {
             dt[u] += bias;
-            if (L < 4) {
-                if (a.softplus) dt[u] = ss_softplus(dt[u]);
-                if (PASS != SCAN_ENDS && a.z) z[u] = ss_silu(z[u]);
+        }
+        // (one branch for the tile's tokens, whose chains of operations then run beside each other)
+        if (a.softplus) {
+            if constexpr (L >= 4) ss_shared(dt, sub, [](float v) { return ss_softplus(v); });
+            else {
+#pragma unroll
+                for (int u = 0; u < TT; ++u) dt[u] = ss_softplus(dt[u]);
             }
         }
-        if constexpr (L >= 4) {
-            // (each of four lanes of a channel works out two tokens' and tells the others)
-            if (a.softplus) ss_shared(dt, sub, [](float v) { return ss_softplus(v); });
-            if (PASS != SCAN_ENDS && a.z) ss_shared(z, sub, [](float v) { return ss_silu(v); });
+        if (PASS != SCAN_ENDS && a.z) {
+            if constexpr (L >= 4) ss_shared(z, sub, [](float v) { return ss_silu(v); });
+            else {
+#pragma unroll
+                for (int u = 0; u < TT; ++u) z[u] = ss_silu(z[u]);
+            }
         }
         if (PASS == SCAN_ENDS) {
 #pragma unroll
@@ -278,14 +293,25 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
 #pragma unroll
             for (int u = 0; u < TT; ++u) {
                 ys[u] = fmaf(dv, x[u], ss_sum<L>(ys[u]));
-                if (a.z) ys[u] *= z[u];
+            }
+            if (a.z) {
+#pragma unroll
+                for (int u = 0; u < TT; ++u) ys[u] *= z[u];
             }
             if (sub == 0 && real) {
                 char* yt = (char*)a.y + t * a.y_stride * (int64_t)sizeof(T);
+                if (left >= TT) {
 #pragma unroll
-                for (int u = 0; u < TT; ++u) {
-                    if (u < left) *(T*)(yt + lane_at) = (T)ys[u];
-                    yt += a.y_stride * (int64_t)sizeof(T);
+                    for (int u = 0; u < TT; ++u) {
+                        *(T*)(yt + lane_at) = (T)ys[u];
+                        yt += a.y_stride * (int64_t)sizeof(T);
+                    }
+                } else {
+#pragma unroll
+                    for (int u = 0; u < TT; ++u) {
+                        if (u < left) *(T*)(yt + lane_at) = (T)ys[u];
+                        yt += a.y_stride * (int64_t)sizeof(T);
+                    }
                 }
             }
         }
@@ -493,15 +519,15 @@ ScanPlan plan_scan(const cadnn_scan_args& g) {
     // (64 sequences x 2048 channels x 16 states, fp16: 1 token 5.8 us here and 8.9 by the kernel for long sequences, 2 tokens 7.1, 9.1, 4 tokens 9.9, 9.7)
     p.few = longest <= 4;
     if (p.few) return p;
-    // A wave alone on its SIMD takes 0.41 us a token, whatever there is beside it on the chip; full, the chip takes 0.67 us for
-    // a token of 1024 waves, both passes over pieces and their join together, which cost 12 us more to begin with.  (One sequence
-    // x 2048 x 16: 64 tokens 29.5 us whole, 20.6 in pieces, 1024 tokens 419, 42; 16 sequences of 64 tokens 30.9, 38.9; 16 x 1024 channels x 64 states, 1024
-    // tokens 445, 588.)
+    // A wave alone on its SIMD takes 0.36 us a token and 3.5 more, whatever there is beside it on the chip; full, the chip takes 0.54 us for
+    // a token of 1024 waves, both passes over pieces and their join together, which cost 12 us more to begin with.  (2048 channels x 16, us whole
+    // and in pieces: one sequence of 64 tokens 26.3, 19.3, of 1024 tokens 368, 37; 4 of 64 tokens 26.9, 22.0; 16 of 256 tokens 96.3, 81.8; 16 of 64 tokens
+    // of 512 channels 26.9, 21.6; 16 x 1024 channels x 64 states, 1024 tokens 413 and by these figures 565.)
     const int64_t blocks = (int64_t)g.groups * p.blocks_per_group;
     p.chunk = 512;
     while (p.chunk > 16 && seq_slots(g.tokens, g.seqs, g.seq_start != nullptr, p.chunk) * blocks * 4 < 2048) p.chunk /= 2;
-    const double whole = 0.41 * longest * (double)((g.seqs * blocks * 4 + 1023) / 1024);
-    const double pieces = 12.0 + std::max(0.67 * (double)g.tokens * (double)(blocks * 4) / 1024.0, 0.82 * p.chunk);
+    const double whole = (3.5 + 0.36 * longest) * (double)((g.seqs * blocks * 4 + 1023) / 1024);
+    const double pieces = 12.0 + std::max(0.54 * (double)g.tokens * (double)(blocks * 4) / 1024.0, 0.72 * p.chunk);
     if (whole <= pieces) {
         p.chunk = 0;
         return p;
