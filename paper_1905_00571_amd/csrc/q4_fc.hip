@@ -231,8 +231,8 @@ __global__ __launch_bounds__(512) void q4_few_kernel(const Q4Args a) {
 // As many tokens as one matrix instruction has columns: 16 in fp16, five in fp32, where the three parts of a token take three
 // columns and one instruction serves all of them.  The workgroup brings the activations of a chunk (one block for every
 // wave) into LDS, each element read, and cut apart, once, while the matrix instructions work on the chunk before, and a wave's
-// codes and scales are fetched D chunks ahead.  us at 8192 -> 8192, groups of 128, one token: fp16 9.6, fp32 12.4, where the kernel above
-// takes 14.0 and 19.7; the 35 MB are 6.4 us at the rate of a large copy.
+// codes and scales are fetched D chunks ahead.  us at 8192 -> 8192, groups of 128, one token: fp16 9.7, fp32 12.3, where the kernel above
+// takes 14.1 and 19.0; the 35 MB are 6.4 us at the rate of a large copy.
 // (Two workgroups to a compute unit, which takes 128 registers: with one, the 257 tiles of 4099 filters took twice the time of 256.)
 template <typename T, int GP, int HELD>
 __global__ __launch_bounds__(512, 4) void q4_columns_kernel(const Q4Args a) {
@@ -359,7 +359,7 @@ hipError_t launch_few(const Q4Args& a, hipStream_t s) {
 // tokens meet all banks.  KS steps of 32 inputs are expanded at a time; their sums start from zero in the first matrix
 // instruction and are multiplied by the group's scale into the fp32 accumulators, which for groups of 32 is as much vector
 // work as there is matrix work.  (With the scale multiplied into the codes, rounded to fp16, 2048 tokens through 4096 -> 8192 took 128 us for
-// any group, where this takes 143, 153 and 180 for groups of 128, 64 and 32; the library's fp16 product takes 114.)  WK = 2: two
+// any group, where this takes 143, 151 and 181 for groups of 128, 64 and 32; the library's fp16 product takes 114.)  WK = 2: two
 // times four waves take the blocks in turn and add up, where there are too few workgroups to wait for each other's loads.
 // DIRECT (fp16): activations go straight to LDS, into the second of two buffers, else through registers.
 template <typename T, int GP, int RW, int BN, int KS, int WK, bool DIRECT>
@@ -582,9 +582,9 @@ struct Q4Cost {
 
 // Which kernel.  Large tiles read and expand less, but a workgroup alone on its compute unit waits out every latency, and one
 // more than fit costs a round; so the kernels are compared by what they were measured to take (random data, 4096 -> 4096, 33 to 2048
-// tokens; groups of 128, 64, 32).  fp16, 128 x 128 / 128 x 64 / 64 x 32 tiles / few tokens: 128 tokens 53, 23, 13.6, 17; 512 tokens 53,
-// 25, 30, 55; 2048 tokens 76, 78, 108, more.  fp32, 256 x 64 / 256 x 32 / 128 x 32 / few tokens: 128 tokens 92, 52, 38, 23; 512 tokens 94, 55, 59, 82;
-// 2048 tokens 200, 216, 218, more.
+// tokens; groups of 128, 64, 32).  fp16, 128 x 128 / 128 x 64 / 64 x 32 tiles / few tokens: 128 tokens 50, 22, 13.7, 15; 512 tokens 51,
+// 25, 29, 52; 2048 tokens 76, 85, 115, more.  fp32, 256 x 64 / 256 x 32 / 128 x 32 / few tokens: 128 tokens 90, 51, 34, 22; 512 tokens 91, 54, 57, 81;
+// 2048 tokens 198, 216, 218, more.
 template <typename T, int GP>
 hipError_t launch_q4(const Q4Args& a, hipStream_t s) {
     auto workgroups = [&](int filters, int tokens) { return (int64_t)((a.cout + filters - 1) / filters) * ((a.n + tokens - 1) / tokens); };
@@ -615,9 +615,9 @@ hipError_t launch_q4(const Q4Args& a, hipStream_t s) {
             if (f2 <= f1 && workgroups(64, 32) >= 256) return launch_few<T, GP, 4, 2>(a, s);
         }
     }
-    // Staged activations pay from rows of some length on (one token, 512 -> 512: fp16 3.5 staged, 2.9 not; 4096 -> 4096: 5.0, 5.9).
+    // Staged activations pay from rows of some length on (one token, 512 -> 512: fp16 3.5 staged, 2.9 not; 4096 -> 4096: 4.5, 5.7).
     if (a.n <= 16 / Q4Frag<T>::kParts && a.blocks > (sizeof(T) == 2 ? 16 : 8)) return launch_columns<T, GP>(a, s);
-    // (13 tokens, 5003 -> 4099, groups of 32, fp16: one tile of filters a wave 22.5, two 14.5; 4096 filters, one 14.6, two 15.9)
+    // (13 tokens, 5003 -> 4099, groups of 32, fp16: one tile of filters a wave 22.5, two 14.5; 4096 filters, one 13.5, two 14.5)
     if (a.n <= 16) return a.cout > 16 * 256 && a.blocks > 8 ? launch_few<T, GP, 2, 1>(a, s) : launch_few<T, GP, 1, 1>(a, s);
     constexpr bool h = sizeof(T) == 2;
     constexpr Q4Cost few1 = {h ? 7.3 : 11.3, h ? 12.5 : 20, 512}, few2 = {h ? 9.3 : 11.8, h ? 13 : 21.5, 512}, few4 = {h ? 11.5 : 16.5, h ? 16.5 : 27, 512};

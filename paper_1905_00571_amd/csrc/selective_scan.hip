@@ -8,7 +8,7 @@
 // SIMD per 64 of them, against 4 / N elements of traffic: from N = 16 on the vector units bound a long scan, and the
 // states' traffic a single token.  A long sequence is a chain of tokens that only channels and states run beside, so it is cut into
 // pieces: one pass for what each piece ends with, a join, one for the outputs -- the exponentials are taken twice.  us at 4096
-// tokens x 2048 channels x 16 states, gated, fp16: 36 + 7 + 44 (two waves a SIMD; 20 for the vector work of one pass at its rate, 12 for the
+// tokens x 2048 channels x 16 states, gated, fp16: 33 + 11 + 41 (four waves a SIMD; 20 for the vector work of one pass at its rate, 12 for the
 // traffic); one token of 64 sequences x 4096 x 16: 11.8, 3.1 TB/s.
 #include <type_traits>
 
@@ -157,50 +157,46 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
         t1 = (int)min((int64_t)hi, first + a.chunk);
     }
     if (t0 >= t1) return;
-    // (rows are uniform, channels are the lanes': a scalar base and a 32-bit offset address a load)
-    const uint32_t lane_at = (uint32_t)ch * (uint32_t)sizeof(T);
-    auto elem = [&](const void* base, int64_t stride, int at) -> T { return *(const T*)((const char*)base + at * stride * (int64_t)sizeof(T) + lane_at); };
+    const uint32_t lane_bytes = (uint32_t)ch * (uint32_t)sizeof(T);
+    // Rows are uniform, channels are the lanes': a scalar base and a 32-bit offset address a load.  (The compiler keeps them so if it does not see
+    // what they are made of; else it adds them up for every lane, 96 instructions a tile.)
+    typedef __attribute__((address_space(1))) char Global;
+    auto here = [&]() -> uint32_t { uint32_t v = lane_bytes; asm volatile("" : "+v"(v)); return v; };
+    auto at_row = [&](const void* base, int64_t stride, int at, uint32_t lane) -> __attribute__((address_space(1))) T* {
+        Global* row = (Global*)((const char*)base + at * stride * (int64_t)sizeof(T));
+        asm volatile("" : "+s"(row));
+        return (__attribute__((address_space(1))) T*)(row + lane);
+    };
     const T* bp = (const T*)a.b + (int64_t)grp * a.dstate;
     const T* cp = (const T*)a.c + (int64_t)grp * a.dstate;
     T nx[TT], nd[TT], nz[TT];
     T nb[PER];
-    auto fetch = [&](int t) {
-        if (t + TT <= t1) {
-            const char *x = (const char*)a.x + t * a.x_stride * (int64_t)sizeof(T), *d = (const char*)a.dt + t * a.dt_stride * (int64_t)sizeof(T);
-            const char* z = a.z ? (const char*)a.z + t * a.z_stride * (int64_t)sizeof(T) : nullptr;
 #pragma unroll
-            for (int u = 0; u < TT; ++u) {
-                nx[u] = *(const T*)(x + lane_at);
-                nd[u] = *(const T*)(d + lane_at);
-                x += a.x_stride * (int64_t)sizeof(T);
-                d += a.dt_stride * (int64_t)sizeof(T);
-            }
-            if (PASS != SCAN_ENDS && z) {
+    for (int u = 0; u < TT; ++u) nz[u] = (T)0.0f;
+    // rows t to t + 7, and rows that lie in front of the sequence as its first one
+    auto fetch = [&](int t, auto whole) {
+        const uint32_t lane = here();
+        auto row = [&](const void* base, int64_t stride, int u) -> T { return *at_row(base, stride, decltype(whole)::value ? t + u : max(t + u, t0), lane); };
 #pragma unroll
-                for (int u = 0; u < TT; ++u) {
-                    nz[u] = *(const T*)(z + lane_at);
-                    z += a.z_stride * (int64_t)sizeof(T);
-                }
-            }
-        } else {
+        for (int u = 0; u < TT; ++u) nx[u] = row(a.x, a.x_stride, u);
 #pragma unroll
-            for (int u = 0; u < TT; ++u) {
-                const int at = min(t + u, t1 - 1);
-                nx[u] = elem(a.x, a.x_stride, at);
-                nd[u] = elem(a.dt, a.dt_stride, at);
-                if (PASS != SCAN_ENDS && a.z) nz[u] = elem(a.z, a.z_stride, at);
-            }
+        for (int u = 0; u < TT; ++u) nd[u] = row(a.dt, a.dt_stride, u);
+        if (PASS != SCAN_ENDS && a.z) {
+#pragma unroll
+            for (int u = 0; u < TT; ++u) nz[u] = row(a.z, a.z_stride, u);
         }
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             const int i = k * 256 + tid, u = i / ROW, r = i % ROW, n = r < N ? r : r - N, at = t + u;
             T v = (T)0.0f;
-            if (i < TT * ROW && at < t1 && n < a.dstate)
+            if (i < TT * ROW && (decltype(whole)::value || at >= t0) && (FULL || n < a.dstate))
                 v = r < N ? bp[(int64_t)at * a.b_stride + n] : cp[(int64_t)at * a.c_stride + n];
             nb[k] = v;
         }
     };
-    fetch(t0);
+    const bool has_whole = t1 - t0 >= TT;
+    if (has_whole) fetch(t0, std::true_type{});
+    else fetch(t1 - TT, std::false_type{});
     float h[NS], al[NS];
     const int n_left = a.dstate - sub * NS;
     float* kept = nullptr;
@@ -218,25 +214,31 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
     const float dv = a.d ? a.d[ch] : 0.0f;
     float span = 0.0f;
     int buf = 0;
-    for (int t = t0; t < t1; t += TT, buf ^= 1) {
+    // The rows t to t + 7 that were fetched; of the last tile, where the sequence does not end with a whole one, they are the
+    // sequence's last eight, and the first `skip` of them are done or in front of it.
+    auto tile = [&](int t, int skip, auto whole) {
+        constexpr bool W = decltype(whole)::value;
         float x[TT], dt[TT], z[TT];
 #pragma unroll
         for (int u = 0; u < TT; ++u) {
             x[u] = (float)nx[u];
             dt[u] = (float)nd[u];
-            z[u] = PASS != SCAN_ENDS && a.z ? (float)nz[u] : 0.0f;
+            if (PASS != SCAN_ENDS) z[u] = (float)nz[u];
+        }
+        // (converted here: put off, the conversions would have the next rows' loads write to other registers, and 24 copies)
+#pragma unroll
+        for (int u = 0; u < TT; ++u) {
+            asm volatile("" : "+v"(x[u]), "+v"(dt[u]));
+            if (PASS != SCAN_ENDS) asm volatile("" : "+v"(z[u]));
         }
 #pragma unroll
         for (int k = 0; k < PER; ++k)
             if (k * 256 + tid < TT * ROW) bc[buf][k * 256 + tid] = nb[k];
         __syncthreads();     // (the other buffer is written next, after the next barrier's readers of this one)
-        if (t + TT < t1) fetch(t + TT);
-        const int left = t1 - t;
+        if (W) fetch(min(t + TT, t1 - TT), std::true_type{});      // (the last one's rows again where nothing follows: no branch parts the tile)
         float steps = 0.0f;          // (summed by tiles: 8 + chunk / 8 roundings at most, not chunk)
 #pragma unroll
-        for (int u = 0; u < TT; ++u) {
-            dt[u] += bias;
-        }
+        for (int u = 0; u < TT; ++u) dt[u] += bias;
         // (one branch for the tile's tokens, whose chains of operations then run beside each other)
         if (a.softplus) {
             if constexpr (L >= 4) ss_shared(dt, sub, [](float v) { return ss_softplus(v); });
@@ -254,7 +256,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
         }
         if (PASS == SCAN_ENDS) {
 #pragma unroll
-            for (int u = 0; u < TT; ++u) steps += u < left ? dt[u] : 0.0f;
+            for (int u = 0; u < TT; ++u) steps += W || u >= skip ? dt[u] : 0.0f;
             span += steps;
         }
         float ys[TT];
@@ -279,43 +281,30 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
             }
             ys[u] = y;
         };
-        if (left >= TT) {
 #pragma unroll
-            for (int u = 0; u < TT; ++u) token(u);
-        } else {
-#pragma unroll
-            for (int u = 0; u < TT; ++u) {
-                ys[u] = 0.0f;
-                if (u < left) token(u);
-            }
+        for (int u = 0; u < TT; ++u) {
+            if (!W) ys[u] = 0.0f;
+            if (W || u >= skip) token(u);
         }
         if (PASS != SCAN_ENDS) {
 #pragma unroll
-            for (int u = 0; u < TT; ++u) {
-                ys[u] = fmaf(dv, x[u], ss_sum<L>(ys[u]));
-            }
+            for (int u = 0; u < TT; ++u) ys[u] = fmaf(dv, x[u], ss_sum<L>(ys[u]));
             if (a.z) {
 #pragma unroll
                 for (int u = 0; u < TT; ++u) ys[u] *= z[u];
             }
             if (sub == 0 && real) {
-                char* yt = (char*)a.y + t * a.y_stride * (int64_t)sizeof(T);
-                if (left >= TT) {
+                const uint32_t lane = here();
 #pragma unroll
-                    for (int u = 0; u < TT; ++u) {
-                        *(T*)(yt + lane_at) = (T)ys[u];
-                        yt += a.y_stride * (int64_t)sizeof(T);
-                    }
-                } else {
-#pragma unroll
-                    for (int u = 0; u < TT; ++u) {
-                        if (u < left) *(T*)(yt + lane_at) = (T)ys[u];
-                        yt += a.y_stride * (int64_t)sizeof(T);
-                    }
-                }
+                for (int u = 0; u < TT; ++u)
+                    if (W || u >= skip) *at_row(a.y, a.y_stride, t + u, lane) = (T)ys[u];
             }
         }
-    }
+        buf ^= 1;
+    };
+    int t = t0;
+    for (; t + TT <= t1; t += TT) tile(t, 0, std::true_type{});
+    if (t < t1) tile(t1 - TT, TT - (t1 - t), std::false_type{});
     if (real && kept && PASS != SCAN_PIECES) {
         ss_store<NS>(kept, FULL ? NS : n_left, h);
         if (PASS == SCAN_ENDS && sub == 0) a.span[slot * a.channels + ch] = span;
@@ -519,15 +508,18 @@ ScanPlan plan_scan(const cadnn_scan_args& g) {
     // (64 sequences x 2048 channels x 16 states, fp16: 1 token 5.8 us here and 8.9 by the kernel for long sequences, 2 tokens 7.1, 9.1, 4 tokens 9.9, 9.7)
     p.few = longest <= 4;
     if (p.few) return p;
-    // A wave alone on its SIMD takes 0.36 us a token and 3.5 more, whatever there is beside it on the chip; full, the chip takes 0.54 us for
+    // A wave alone on its SIMD takes 0.36 us a token and 3.5 more, whatever there is beside it on the chip; full, the chip takes 0.5 us for
     // a token of 1024 waves, both passes over pieces and their join together, which cost 12 us more to begin with.  (2048 channels x 16, us whole
-    // and in pieces: one sequence of 64 tokens 26.3, 19.3, of 1024 tokens 368, 37; 4 of 64 tokens 26.9, 22.0; 16 of 256 tokens 96.3, 81.8; 16 of 64 tokens
-    // of 512 channels 26.9, 21.6; 16 x 1024 channels x 64 states, 1024 tokens 413 and by these figures 565.)
+    // and in pieces: one sequence of 64 tokens 26.8, 20.5, of 1024 tokens 371, 37; 4 of 64 tokens 27.2, 23.0; 16 of 256 tokens 98, 81; 16 of 64 tokens
+    // of 512 channels 27.2, 22.6; 16 x 1024 channels x 64 states, 1024 tokens 413 and by these figures 524.)
+    // Pieces are the longest that make 2560 waves, for up to four of a SIMD; more of them cost the join what they give the passes (us at 4096 x 2048 x 16,
+    // fp16, passes and join: pieces of 64 tokens 35.5 + 44.9 + 6.6, of 32 tokens 32.7 + 41.0 + 11.4; 1501 x 1000 x 64, fp32, 9 sequences: 64 tokens 32.0 + 39.1 +
+    // 7.3, 32 tokens 28.9 + 33.8 + 9.3, 16 tokens 27.3 + 31.5 + 35).
     const int64_t blocks = (int64_t)g.groups * p.blocks_per_group;
     p.chunk = 512;
-    while (p.chunk > 16 && seq_slots(g.tokens, g.seqs, g.seq_start != nullptr, p.chunk) * blocks * 4 < 2048) p.chunk /= 2;
+    while (p.chunk > 16 && seq_slots(g.tokens, g.seqs, g.seq_start != nullptr, p.chunk) * blocks * 4 < 2560) p.chunk /= 2;
     const double whole = (3.5 + 0.36 * longest) * (double)((g.seqs * blocks * 4 + 1023) / 1024);
-    const double pieces = 12.0 + std::max(0.54 * (double)g.tokens * (double)(blocks * 4) / 1024.0, 0.72 * p.chunk);
+    const double pieces = 12.0 + std::max(0.5 * (double)g.tokens * (double)(blocks * 4) / 1024.0, 0.72 * p.chunk);
     if (whole <= pieces) {
         p.chunk = 0;
         return p;
