@@ -311,6 +311,10 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
     }
 }
 
+// What a piece ends with that starts from h.  (Where a is positive a piece's factor may pass what fp32 holds though none of its steps does: a state of
+// zero stays out of it.)
+__device__ __forceinline__ float ss_after(float f, float h, float end) { return h == 0.0f ? end : fmaf(f, h, end); }
+
 // Joins the pieces of each sequence, h = exp(a * span) * h + end; what a piece ended with is replaced by what it starts from.
 // A workgroup owns 64 (channel, state) pairs of a sequence.  Its four waves fetch S pieces each, join them from zero, learn
 // from each other what they start from, and go through them again, in registers: the chain of a long sequence costs one
@@ -332,7 +336,7 @@ __device__ __forceinline__ float ss_join(const SsArgs& a, int64_t per_seq, int64
     for (int u = 0; u < S; ++u) {
         // (not below the smallest normal number: an infinite state outlives any number of steps that each shrink it a little)
         f[u] = fmaxf(ss_exp2(al * f[u]), 0x1p-126f);
-        own = fmaf(f[u], own, end[u]);
+        own = ss_after(f[u], own, end[u]);
         all = fmaxf(all * f[u], 0x1p-126f);
     }
     lds[0][wave][lane] = all;
@@ -342,13 +346,13 @@ __device__ __forceinline__ float ss_join(const SsArgs& a, int64_t per_seq, int64
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         if (w == wave) mine = h;
-        h = fmaf(lds[0][w][lane], h, lds[1][w][lane]);
+        h = ss_after(lds[0][w][lane], h, lds[1][w][lane]);
     }
 #pragma unroll
     for (int u = 0; u < S; ++u) {
         const int p = p0 + wave * S + u;
         if (p < pieces && first + p < a.slots) a.part[(first + p) * per_seq + i] = mine;
-        mine = fmaf(f[u], mine, end[u]);
+        mine = ss_after(f[u], mine, end[u]);
     }
     __syncthreads();
     return h;
@@ -404,7 +408,7 @@ __global__ __launch_bounds__(256) void scan_join_few_kernel(const SsArgs a) {
         for (int u = 0; u < U; ++u)
             if (p + u < pieces) {
                 part[u * per_seq] = h;
-                h = fmaf(fmaxf(ss_exp2(al * f[u]), 0x1p-126f), h, end[u]);
+                h = ss_after(fmaxf(ss_exp2(al * f[u]), 0x1p-126f), h, end[u]);
             }
         part += U * per_seq;
         span += (int64_t)U * a.channels;

@@ -317,6 +317,35 @@ def test_selective_scan_with_masked_steps_and_values_that_are_not_finite(tokens,
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("lens", [[100], [1000], [90, 1000]])
+def test_selective_scan_with_states_that_grow(lens):
+    """a > 0: over a run of rows exp(a * steps) passes what fp32 holds, but states that are zero until the last rows do not notice."""
+    v = scan_inputs(lens, 20, 16, 1, np.float32, 12)
+    v["a"] = np.abs(v["a"]) * 0.25
+    v["dt"][:] = 8.0
+    v["state"][:] = 0.0
+    starts = starts_of(lens)
+    for lo, hi in zip(starts, starts[1:]):
+        v["x"][lo:hi - 3] = 0.0
+    ref, bound, last, off = scan_reference(v, starts, False, False, False)
+    y, kept = run_scan(v, dev(starts), len(lens), False, False, False)
+    check(y, ref, bound, "f32")
+    check(kept, last, off, "f32")
+
+
+@pytest.mark.gpu
+def test_selective_scan_of_a_long_sequence():
+    """More pieces of one sequence than are joined in one round."""
+    for tokens in (2065, 5000):
+        v = scan_inputs([tokens], 6, 16, 1, np.float32, tokens)
+        v["a"] *= 0.01                  # (what a row leaves is still there thousands of rows later)
+        ref, bound, last, off = scan_reference(v, [0, tokens], True, True)
+        y, kept = run_scan(v, None, 1)
+        check(y, ref, bound, "f32")
+        check(kept, last, off, "f32")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("tokens", [12, 400, 3000])
 def test_selective_scan_cuts_bad_offsets(tokens):
     """Offsets that lie outside the rows or descend change no row and no state but those of the call's own tensors."""
