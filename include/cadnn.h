@@ -208,7 +208,8 @@ cadnn_status cadnn_q4_fc(const cadnn_q4_weights* w, const void* x, int64_t x_str
  * seq_start: DEVICE array of seqs + 1 ascending offsets -- sequence s is rows seq_start[s] up to
  * seq_start[s + 1] -- or NULL: every sequence has tokens / seqs rows.  Sequences may be empty (their state
  * is left alone), and rows that belong to none are neither read into an output nor written.  The offsets are read on the device, in
- * stream order; values outside [0, tokens] are cut to it, and an end before its start is an empty sequence.
+ * stream order; values outside [0, tokens] are cut to it.  That they ascend is the caller's part: where they do not, nothing
+ * outside the call's tensors is touched, but which rows and states are written, and with what, is not defined.
  * Rows lie `*_stride` elements apart.  tokens = 0 is a call that does nothing.
  * A state is kept by the caller, one per sequence, read when the call begins and replaced by what the
  * sequence ends with: a prompt in one call, in several, or token by token leads to the same values.  NULL: every
