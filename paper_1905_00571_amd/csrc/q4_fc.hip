@@ -231,14 +231,15 @@ __global__ __launch_bounds__(512) void q4_few_kernel(const Q4Args a) {
 // As many tokens as one matrix instruction has columns: 16 in fp16, five in fp32, where the three parts of a token take three
 // columns and one instruction serves all of them.  The workgroup brings the activations of a chunk (one block for every
 // wave) into LDS, each element read, and cut apart, once, while the matrix instructions work on the chunk before, and a wave's
-// codes and scales are fetched D chunks ahead.  us at 8192 -> 8192, groups of 128, one token: fp16 9.7, fp32 12.3, where the kernel above
-// takes 14.1 and 19.0; the 35 MB are 6.4 us at the rate of a large copy.
+// codes and scales are fetched D chunks ahead.  us at 8192 -> 8192, groups of 128, one token: fp16 8.9, fp32 11.8, where the kernel above
+// takes 14.1 and 19.0; the 35 MB are 6.4 us at the rate of a large copy.  (Fetched 3, 4, 8 chunks ahead, which repeats the last block as often behind the
+// end: fp16 9.4, 9.8, 11.7; not fetched there, by a branch: 9.7, as what is waited for is then less well known.)
 // (Two workgroups to a compute unit, which takes 128 registers: with one, the 257 tiles of 4099 filters took twice the time of 256.)
 template <typename T, int GP, int HELD>
 __global__ __launch_bounds__(512, 4) void q4_columns_kernel(const Q4Args a) {
     typedef Q4Frag<T> F;
     constexpr int P = F::kParts;
-    constexpr int D = 4;
+    constexpr int D = 2;
 
     extern __shared__ __attribute__((aligned(16))) char q4_smem[];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = (int)blockDim.x >> 6;
@@ -615,7 +616,7 @@ hipError_t launch_q4(const Q4Args& a, hipStream_t s) {
             if (f2 <= f1 && workgroups(64, 32) >= 256) return launch_few<T, GP, 4, 2>(a, s);
         }
     }
-    // Staged activations pay from rows of some length on (one token, 512 -> 512: fp16 3.5 staged, 2.9 not; 4096 -> 4096: 4.5, 5.7).
+    // Staged activations pay from rows of some length on (one token, 512 -> 512: fp16 3.5 staged, 2.9 not; 4096 -> 4096: 4.3, 5.7).
     if (a.n <= 16 / Q4Frag<T>::kParts && a.blocks > (sizeof(T) == 2 ? 16 : 8)) return launch_columns<T, GP>(a, s);
     // (13 tokens, 5003 -> 4099, groups of 32, fp16: one tile of filters a wave 22.5, two 14.5; 4096 filters, one 13.5, two 14.5)
     if (a.n <= 16) return a.cout > 16 * 256 && a.blocks > 8 ? launch_few<T, GP, 2, 1>(a, s) : launch_few<T, GP, 1, 1>(a, s);
