@@ -29,11 +29,12 @@ cadnn_status launch_q4_fc(const cadnn_q4_weights* w, const void* x, int64_t x_st
 // not be captured while memory is still to be allocated (NULL: none).
 cadnn_status ensure_q4_device(const cadnn_q4_weights* w, const char* who, hipStream_t capturing, bool has_stream);
 
-// v / (1 + exp(-v)), to about 6 half steps of the value: the exponent's product with log2(e) is taken in two parts, so that its
-// rounding does not grow with v.  (Below -150, where the quotient is zero, the parts could be infinite.)  A third of the
-// instructions of the library's exponential and quotient, which bounded the fp16 convolution.
+// v / (1 + exp(-v)), to about 6 half steps of the value (from -87 on; below, where exp(-v) passes what fp32 holds, to 1e-36): the exponent's
+// product with log2(e) is taken in two parts, so that its rounding does not grow with v.  (Beyond 150 on either side, where the exponential is 0 or the
+// quotient is, the parts could be infinite and their difference no number.)  A third of the instructions of the library's exponential and quotient,
+// which bounded the fp16 convolution.
 __device__ __forceinline__ float act_silu(float v) {
-    const float u = v < -150.0f ? 150.0f : -v;
+    const float u = __builtin_amdgcn_fmed3f(-v, -150.0f, 150.0f);
     const float hi = u * 1.44269502f, lo = fmaf(u, 1.44269502f, -hi) + u * 1.92596303e-8f;
     const float e = __builtin_amdgcn_exp2f(hi);
     return v * __builtin_amdgcn_rcpf(fmaf(e, fmaf(lo, 0.693147182f, 1.0f), 1.0f));

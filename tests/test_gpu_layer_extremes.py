@@ -1,0 +1,59 @@
+"""Sequence layers and 4-bit products at the ends of their values' and sizes' range: activations and weights that overflow, states
+that grow or vanish by more than fp32 holds on the way, numbers of sequences beyond what one launch takes.
+
+The bounds of finite results are those of the layers' own tests (test_gpu_q4.py, test_gpu_sequence.py)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1905_00571_amd as cad
+from test_gpu_sequence import TYPES, U, dev, half_step
+
+# ---- SiLU -----------------------------------------------------------------------------------------
+
+ENDS = np.array([np.inf, np.finfo(np.float32).max, 3e38, 2.4e38, 2.3e38, 6e4, 1e4, 151.0, 150.0, 149.0, 88.0, 17.0, 1.0, 0.0, -0.0, -1e-3, -1.0, -20.0, -80.0,
+                 -149.0, -150.0, -151.0, -6e4, -2.4e38, np.finfo(np.float32).min, -np.inf, np.nan], np.float32)
+
+
+def check_silu(y, v, dtype):
+    """y of v / (1 + exp(-v)): no numbers and infinities where that has them in 64 bits, rounded to the type; a finite value to 8 half steps of
+    fp32 (and, below 2^-100, to 1e-30)."""
+    with np.errstate(all="ignore"):
+        ref = v.astype(np.float64) / (1 + np.exp(-v.astype(np.float64)))
+        held = ref.astype(np.float16 if dtype == "f16" else np.float32)
+    got = y.double().cpu().numpy()
+    assert np.array_equal(np.isnan(got), np.isnan(ref)), (got, ref)
+    infinite = np.isinf(held)
+    assert np.array_equal(got[infinite], held[infinite].astype(np.float64))
+    f = np.isfinite(held)
+    assert (np.abs(got[f] - ref[f]) <= 8 * U * np.abs(ref[f]) + half_step(ref[f], dtype) + 1e-30).all(), (got, ref)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("n,cin", [(1, 64), (1, 2304), (20, 64), (300, 64)])
+def test_silu_of_a_product_at_the_ends_of_its_range(dtype, n, cin):
+    tt, flag, _ = TYPES[dtype]
+    h = cad.cadnn_q4_pack_codes(np.ones((len(ENDS), cin), np.int8), np.ones((len(ENDS), -(-cin // 32)), np.float32), 32, flag)
+    x = torch.zeros(n, cin, dtype=tt, device="cuda")
+    y = cad.cadnn_q4_fc(h, x, dev(ENDS), cad.ACT_SILU)
+    for row in {0, n // 2, n - 1}:
+        check_silu(y[row], ENDS, dtype)
+    x[0, 3] = float("inf")                  # an activation that has overflowed
+    y = cad.cadnn_q4_fc(h, x, None, cad.ACT_SILU)
+    assert bool((y[0] == float("inf")).all()) and bool((y[1:] == 0).all())
+    h.free()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("channels", [1, 16])
+def test_silu_of_a_convolution_at_the_ends_of_its_range(dtype, channels):
+    tt, flag, npt = TYPES[dtype]
+    with np.errstate(over="ignore"):
+        x = np.repeat(ENDS.astype(npt)[:, None], channels, 1)
+    for w in (np.ones((channels, 1, 1, 1), np.float32), np.tile(np.float32([0, 1]), (channels, 1)).reshape(channels, 1, 1, 2)):      # (all taps, a tap of zero)
+        h = cad.cadnn_pack_weights(w, flag)
+        y = cad.cadnn_causal_conv1d(h, dev(x), act=cad.ACT_SILU)
+        check_silu(y, x.astype(np.float32), dtype)
+        h.free()
