@@ -243,7 +243,8 @@ cadnn_status cadnn_causal_conv1d(const cadnn_weights* w, const void* x, int64_t 
  * memory of the current device.
  * workspace: device memory of cadnn_selective_scan_workspace_bytes bytes (0 for many calls, and always for single tokens), used by this call alone until it is through: long
  * sequences that are too few to fill the chip are cut into pieces that run side by side.  Without it, or with
- * less, every sequence is worked on from end to end: slower, and with differently rounded sums.
+ * less, every sequence is worked on from end to end: slower, and with differently rounded sums.  (A state that passes what fp32 holds and
+ * would come back, by rows that shrink it, stays infinite from end to end; in pieces it may come back.)
  * Errors: EINVAL (NULL pointer, bad sizes or strides as above, channels that are no multiple of groups, a
  * misaligned pointer, unknown dtype, negative longest); EUNSUPPORTED (dstate above 256, more than 2^20 channels, 4096 groups, 65535 sequences or
  * 2^30 tokens); EHIP. */

@@ -311,9 +311,21 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
     }
 }
 
-// What a piece ends with that starts from h.  (Where a is positive a piece's factor may pass what fp32 holds though none of its steps does: a state of
-// zero stays out of it.)
-__device__ __forceinline__ float ss_after(float f, float h, float end) { return h == 0.0f ? end : fmaf(f, h, end); }
+// 2^e as m * 2^n, for what a piece's steps, whose exponents add up to e, make of a state: 2^e itself may pass what fp32 holds, or vanish, where the
+// state's product with it does neither.  m lies between 1/2 and 2, so that a state of zero stays zero and an infinite one infinite, as after any number of
+// steps that each shrink it a little.  (Beyond 277 every product is zero or infinite.  Where e is no number, what the piece ends with is none either.)
+struct SsFactor {
+    float m;
+    int n;
+};
+__device__ __forceinline__ SsFactor ss_factor(float e) {
+    e = __builtin_amdgcn_fmed3f(e, -400.0f, 400.0f);
+    const float n = truncf(e);
+    return {ss_exp2(e - n), (int)n};
+}
+
+// What a piece ends with that starts from h and, from zero, ends with `end`.
+__device__ __forceinline__ float ss_after(SsFactor f, float h, float end) { return __builtin_amdgcn_ldexpf(f.m * h, f.n) + end; }
 
 // Joins the pieces of each sequence, h = exp(a * span) * h + end; what a piece ended with is replaced by what it starts from.
 // A workgroup owns 64 (channel, state) pairs of a sequence.  Its four waves fetch S pieces each, join them from zero, learn
@@ -322,22 +334,22 @@ __device__ __forceinline__ float ss_after(float f, float h, float end) { return 
 template <int S>
 __device__ __forceinline__ float ss_join(const SsArgs& a, int64_t per_seq, int64_t i, int ch, int64_t first, int p0, int pieces, float al, float h, float (&lds)[2][4][64]) {
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-    float end[S], f[S];
+    float end[S], span[S];
 #pragma unroll
     for (int u = 0; u < S; ++u) {
         const int p = p0 + wave * S + u;
         const int64_t slot = first + min(p, pieces - 1);
         const bool there = p < pieces && slot < a.slots;
         end[u] = there ? a.part[slot * per_seq + i] : 0.0f;
-        f[u] = there ? a.span[slot * a.channels + ch] : 0.0f;
+        span[u] = there ? a.span[slot * a.channels + ch] : 0.0f;
     }
-    float all = 1.0f, own = 0.0f;
+    SsFactor f[S];
+    float all = 0.0f, own = 0.0f;       // of the wave's pieces together: steps are added up, as the product of factors could pass fp32 on its way
 #pragma unroll
     for (int u = 0; u < S; ++u) {
-        // (not below the smallest normal number: an infinite state outlives any number of steps that each shrink it a little)
-        f[u] = fmaxf(ss_exp2(al * f[u]), 0x1p-126f);
+        f[u] = ss_factor(al * span[u]);
         own = ss_after(f[u], own, end[u]);
-        all = fmaxf(all * f[u], 0x1p-126f);
+        all += span[u];
     }
     lds[0][wave][lane] = all;
     lds[1][wave][lane] = own;
@@ -346,7 +358,7 @@ __device__ __forceinline__ float ss_join(const SsArgs& a, int64_t per_seq, int64
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         if (w == wave) mine = h;
-        h = ss_after(lds[0][w][lane], h, lds[1][w][lane]);
+        h = ss_after(ss_factor(al * lds[0][w][lane]), h, lds[1][w][lane]);
     }
 #pragma unroll
     for (int u = 0; u < S; ++u) {
@@ -397,18 +409,18 @@ __global__ __launch_bounds__(256) void scan_join_few_kernel(const SsArgs a) {
     const float* span = a.span + first * a.channels + ch;
     constexpr int U = 4;
     for (int p = 0; p < pieces; p += U) {
-        float end[U] = {}, f[U] = {};
+        float end[U] = {}, steps[U] = {};
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (p + u < pieces) {
                 end[u] = part[u * per_seq];
-                f[u] = span[(int64_t)u * a.channels];
+                steps[u] = span[(int64_t)u * a.channels];
             }
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (p + u < pieces) {
                 part[u * per_seq] = h;
-                h = ss_after(fmaxf(ss_exp2(al * f[u]), 0x1p-126f), h, end[u]);
+                h = ss_after(ss_factor(al * steps[u]), h, end[u]);
             }
         part += U * per_seq;
         span += (int64_t)U * a.channels;

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import paper_1905_00571_amd as cad
-from test_gpu_sequence import TYPES, U, dev, half_step
+from test_gpu_sequence import TYPES, U, check, dev, half_step, run_scan, scan_inputs, scan_reference, starts_of
 
 # ---- SiLU -----------------------------------------------------------------------------------------
 
@@ -57,3 +57,63 @@ def test_silu_of_a_convolution_at_the_ends_of_its_range(dtype, channels):
         y = cad.cadnn_causal_conv1d(h, dev(x), act=cad.ACT_SILU)
         check_silu(y, x.astype(np.float32), dtype)
         h.free()
+
+
+# ---- states that grow and vanish ---------------------------------------------------------------------
+
+LENS = [[200], [400], [900], [2100], [200, 1500]]
+
+
+def check_with_and_without_pieces(v, lens, softplus):
+    starts = starts_of(lens)
+    ref, bound, last, off = scan_reference(v, starts, softplus, True, False)
+    for how in ({}, {"longest": max(lens)}, {"workspace": torch.empty(0, dtype=torch.uint8, device="cuda")}):
+        y, kept = run_scan(v, dev(starts), len(lens), softplus, True, False, **how)
+        check(kept, last, off, "f32", f"state, {lens}, {list(how)}")
+        check(y, ref, bound, "f32", f"{lens}, {list(how)}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", LENS)
+@pytest.mark.parametrize("rows", [16, 64])
+def test_small_states_that_grow_by_more_than_fp32_holds(lens, rows):
+    """States of 1e-30 times exp(110) to exp(128), over 16 rows and over 64 (rows of one piece, and of several)."""
+    v = scan_inputs(lens, 20, 16, 1, np.float32, 13)
+    v["a"] = (v["a"] * 0.0 + np.random.default_rng(1).uniform(110, 128, v["a"].shape) / 128).astype(np.float32)
+    v["x"][:] = 0.0
+    v["dt"][:] = 0.0
+    for lo in starts_of(lens)[:-1]:
+        v["dt"][lo + 96:lo + 96 + rows] = 128.0 / rows
+    v["state"] *= 1e-30
+    check_with_and_without_pieces(v, lens, False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", LENS)
+@pytest.mark.parametrize("first", [1.0, 1e20])
+def test_states_that_vanish_stay_so_when_later_rows_grow(lens, first):
+    """A factor of exp(-256), over 32 rows, and then one of exp(128) over as many: nothing is left of the state."""
+    v = scan_inputs(lens, 20, 16, 1, np.float32, 14)
+    v["a"][:] = -1.0
+    v["x"][:] = 0.0
+    v["dt"][:] = 0.0
+    for lo in starts_of(lens)[:-1]:
+        v["dt"][lo + 16:lo + 48] = 8.0
+        v["dt"][lo + 64:lo + 96] = -4.0
+    v["state"] *= first
+    check_with_and_without_pieces(v, lens, False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", LENS)
+def test_large_states_that_vanish(lens):
+    """States of 1e36 (times ten, outputs would pass what fp32 holds by themselves: sums over the states up to 2e37 and gates up to 5)."""
+    v = scan_inputs(lens, 20, 16, 1, np.float32, 15)
+    v["a"][:] = -1.0
+    v["dt"][:] = 0.0
+    for lo, hi in zip(starts_of(lens), starts_of(lens)[1:]):
+        v["dt"][lo + 16:lo + 48] = 8.0
+        v["x"][lo:lo + 100] = 0.0
+        v["dt"][lo + 100:hi] = 0.1
+    v["state"] *= 1e36
+    check_with_and_without_pieces(v, lens, False)
