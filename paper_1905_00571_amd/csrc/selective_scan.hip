@@ -37,6 +37,9 @@ struct SsArgs {
 
 __device__ __forceinline__ float ss_exp2(float v) { return __builtin_amdgcn_exp2f(v); }
 
+// step * log2(e), for exp(step * a) = exp2(step * log2(e) * a): a stays as it is, so that a step of zero keeps the state whatever finite value a has.
+__device__ __forceinline__ float ss_base2(float step) { return step * 1.44269502f; }
+
 // log(1 + exp(v)) = max(v, 0) + log1p(e), e = exp(-|v|), from the product |v| * log2(e) in two parts.  log1p(e) = e + e^2 q(e), whose q of
 // degree 8 was fitted to it for 0 <= e <= 1 (relative error 2^-27, 1.4 * 2^-24 with the roundings of its evaluation).
 __device__ __forceinline__ float ss_softplus(float v) {
@@ -197,19 +200,17 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
     const bool has_whole = t1 - t0 >= TT;
     if (has_whole) fetch(t0, std::true_type{});
     else fetch(t1 - TT, std::false_type{});
-    float h[NS], al[NS];
+    float h[NS], rate[NS];
     const int n_left = a.dstate - sub * NS;
     float* kept = nullptr;
     if (PASS == SCAN_WHOLE) kept = a.state ? a.state + ((int64_t)s * a.channels + ch) * a.dstate + sub * NS : nullptr;
     else kept = a.part + (slot * a.channels + ch) * a.dstate + sub * NS;
-    ss_load<NS>(a.a + (int64_t)ch * a.dstate + sub * NS, FULL ? NS : n_left, al);
+    ss_load<NS>(a.a + (int64_t)ch * a.dstate + sub * NS, FULL ? NS : n_left, rate);
     if (PASS != SCAN_ENDS && kept) ss_load<NS>(kept, FULL ? NS : n_left, h);
     else {
 #pragma unroll
         for (int k = 0; k < NS; ++k) h[k] = 0.0f;
     }
-#pragma unroll
-    for (int k = 0; k < NS; ++k) al[k] *= 1.44269502f;
     const float bias = a.dt_bias ? a.dt_bias[ch] : 0.0f;
     const float dv = a.d ? a.d[ch] : 0.0f;
     float span = 0.0f;
@@ -263,7 +264,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
         // (outputs are stored behind the tile: a store under a condition would part the tokens' work from each other)
         // one token: three full-rate operations a state beside the exponential and the product under it
         auto token = [&](int u) {
-            const float step = dt[u], in = step * x[u];
+            const float step = ss_base2(dt[u]), in = dt[u] * x[u];
             const T* row = bc[buf] + u * ROW + sub * NS;
             float y = 0.0f;
 #pragma unroll
@@ -274,7 +275,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsArgs a) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     const int k = k0 + e;
-                    h[k] = fmaf((float)bv[e], in, ss_exp2(step * al[k]) * h[k]);
+                    h[k] = fmaf((float)bv[e], in, ss_exp2(step * rate[k]) * h[k]);
                     if (!FULL) h[k] = sub * NS + k < a.dstate ? h[k] : 0.0f;
                     if (PASS != SCAN_ENDS) y = fmaf((float)cv[e], h[k], y);
                 }
@@ -332,7 +333,7 @@ __device__ __forceinline__ float ss_after(SsFactor f, float h, float end) { retu
 // from each other what they start from, and go through them again, in registers: the chain of a long sequence costs one
 // round trip to memory for 4 * S pieces.  (64 pieces of 32768 pairs: 12.5 us with one thread for a pair's whole chain, 9.8 with S = 32, 6.6 with S = 16.)
 template <int S>
-__device__ __forceinline__ float ss_join(const SsArgs& a, int64_t per_seq, int64_t i, int ch, int64_t first, int p0, int pieces, float al, float h, float (&lds)[2][4][64]) {
+__device__ __forceinline__ float ss_join(const SsArgs& a, int64_t per_seq, int64_t i, int ch, int64_t first, int p0, int pieces, float rate, float h, float (&lds)[2][4][64]) {
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
     float end[S], span[S];
 #pragma unroll
@@ -347,7 +348,7 @@ __device__ __forceinline__ float ss_join(const SsArgs& a, int64_t per_seq, int64
     float all = 0.0f, own = 0.0f;       // of the wave's pieces together: steps are added up, as the product of factors could pass fp32 on its way
 #pragma unroll
     for (int u = 0; u < S; ++u) {
-        f[u] = ss_factor(al * span[u]);
+        f[u] = ss_factor(rate * ss_base2(span[u]));
         own = ss_after(f[u], own, end[u]);
         all += span[u];
     }
@@ -358,7 +359,7 @@ __device__ __forceinline__ float ss_join(const SsArgs& a, int64_t per_seq, int64
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         if (w == wave) mine = h;
-        h = ss_after(ss_factor(al * lds[0][w][lane]), h, lds[1][w][lane]);
+        h = ss_after(ss_factor(rate * ss_base2(lds[0][w][lane])), h, lds[1][w][lane]);
     }
 #pragma unroll
     for (int u = 0; u < S; ++u) {
@@ -381,13 +382,13 @@ __global__ __launch_bounds__(256) void scan_join_kernel(const SsArgs a) {
     const int ch = (int)(i / a.dstate);
     const int64_t first = seq_first_slot(a.q, s, a.chunk);
     const int pieces = (int)(((int64_t)hi - lo + a.chunk - 1) / a.chunk);
-    const float al = a.a[i] * 1.44269502f;
+    const float rate = a.a[i];
     float* kept = a.state ? a.state + (int64_t)s * per_seq + i : nullptr;
     float h = kept ? *kept : 0.0f;
     int p = 0;
-    for (; pieces - p > 64; p += 128) h = ss_join<32>(a, per_seq, i, ch, first, p, pieces, al, h, lds);
-    for (; pieces - p > 32; p += 64) h = ss_join<16>(a, per_seq, i, ch, first, p, pieces, al, h, lds);
-    for (; p < pieces; p += 32) h = ss_join<8>(a, per_seq, i, ch, first, p, pieces, al, h, lds);
+    for (; pieces - p > 64; p += 128) h = ss_join<32>(a, per_seq, i, ch, first, p, pieces, rate, h, lds);
+    for (; pieces - p > 32; p += 64) h = ss_join<16>(a, per_seq, i, ch, first, p, pieces, rate, h, lds);
+    for (; p < pieces; p += 32) h = ss_join<8>(a, per_seq, i, ch, first, p, pieces, rate, h, lds);
     if (kept && at < per_seq && threadIdx.x < 64) *kept = h;
 }
 
@@ -402,7 +403,7 @@ __global__ __launch_bounds__(256) void scan_join_few_kernel(const SsArgs a) {
     const int ch = (int)(i / a.dstate);
     const int64_t first = seq_first_slot(a.q, s, a.chunk);
     const int pieces = (int)min(((int64_t)hi - lo + a.chunk - 1) / a.chunk, a.slots - first);
-    const float al = a.a[i] * 1.44269502f;
+    const float rate = a.a[i];
     float* kept = a.state ? a.state + (int64_t)s * per_seq + i : nullptr;
     float h = kept ? *kept : 0.0f;
     float* part = a.part + first * per_seq + i;
@@ -420,7 +421,7 @@ __global__ __launch_bounds__(256) void scan_join_few_kernel(const SsArgs a) {
         for (int u = 0; u < U; ++u)
             if (p + u < pieces) {
                 part[u * per_seq] = h;
-                h = ss_after(ss_factor(al * steps[u]), h, end[u]);
+                h = ss_after(ss_factor(rate * ss_base2(steps[u])), h, end[u]);
             }
         part += U * per_seq;
         span += (int64_t)U * a.channels;
@@ -443,18 +444,16 @@ __global__ __launch_bounds__(256) void scan_few_kernel(const SsArgs a) {
     if (lo >= hi) return;
     const int grp = a.groups == 1 ? 0 : ch / a.per;
     const int left = min(4, a.dstate - n0);       // states of the lane that exist, none or fewer for the last lanes
-    float h[4], al[4];
+    float h[4], rate[4];
     float* kept = a.state ? a.state + ((int64_t)s * a.channels + ch) * a.dstate + n0 : nullptr;
     if (kept) ss_load<4>(kept, left, h);
     else {
 #pragma unroll
         for (int k = 0; k < 4; ++k) h[k] = 0.0f;
     }
-    ss_load<4>(a.a + (int64_t)ch * a.dstate + n0, left, al);
+    ss_load<4>(a.a + (int64_t)ch * a.dstate + n0, left, rate);
     const float bias = a.dt_bias ? a.dt_bias[ch] : 0.0f;
     const float dv = a.d ? a.d[ch] : 0.0f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) al[k] *= 1.44269502f;
     for (int t = lo; t < hi; ++t) {
         const float x = (float)((const T*)a.x)[(int64_t)t * a.x_stride + ch];
         float step = (float)((const T*)a.dt)[(int64_t)t * a.dt_stride + ch] + bias;
@@ -475,10 +474,11 @@ __global__ __launch_bounds__(256) void scan_few_kernel(const SsArgs a) {
         }
         if (a.softplus) step = ss_softplus(step);
         const float in = step * x;
+        step = ss_base2(step);
         float y = 0.0f;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            h[k] = k < left ? fmaf(bv[k], in, ss_exp2(step * al[k]) * h[k]) : 0.0f;
+            h[k] = k < left ? fmaf(bv[k], in, ss_exp2(step * rate[k]) * h[k]) : 0.0f;
             y = fmaf(cv[k], h[k], y);
         }
         y = ss_sum<L>(y);

@@ -117,3 +117,30 @@ def test_large_states_that_vanish(lens):
         v["dt"][lo + 100:hi] = 0.1
     v["state"] *= 1e36
     check_with_and_without_pieces(v, lens, False)
+
+
+# ---- decay rates of the largest magnitude --------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", [[2], [1, 3, 0, 2], [300], [40, 500]])
+def test_rates_of_the_lowest_value(lens):
+    """a of the type's lowest value: a state is forgotten by a row with a step, and kept by one whose step is zero."""
+    v = scan_inputs(lens, 36, 24, 1, np.float32, 16)
+    v["a"][::3] = np.finfo(np.float32).min
+    v["a"][1, ::2] = -2.0 ** 127
+    v["dt"][::2] = -np.inf                    # (softplus gives zero)
+    starts = starts_of(lens)
+    f = {k: a.copy() for k, a in v.items()}
+    f["dt"][::2] = -300.0
+    ref, bound, last, off = scan_reference(f, starts, True, True, False)
+    for how in ({}, {"longest": max(lens)}, {"workspace": torch.empty(0, dtype=torch.uint8, device="cuda")}):
+        y, kept = run_scan(v, dev(starts), len(lens), True, True, False, **how)
+        check(y, ref, bound, "f32", str(how))
+        check(kept, last, off, "f32", str(how))
+        w = dict(v, a=v["a"].copy())
+        w["a"][5, 3] = np.nan
+        z, held = run_scan(w, dev(starts), len(lens), True, True, False, **how)
+        ran = [s for s, m in enumerate(lens) if m]
+        assert bool(torch.isnan(z[:, 5]).all()) and bool(torch.isnan(held[ran, 5, 3]).all())
+        z[:, 5], held[:, 5, 3] = y[:, 5], kept[:, 5, 3]
+        assert torch.equal(y, z) and torch.equal(kept, held)
