@@ -71,12 +71,13 @@ template <> struct Q4Frag<float> {
         return r.v8;
     }
     // The parts are cut off, not rounded, so that a large value's first part stays finite; what is left of an infinity
-    // (no number) is replaced by a finite value that the infinity swallows.
+    // (no number) is replaced by a finite value that the infinity swallows.  A no-number that keeps its payload in its low bits, all of them
+    // signalling, would be cut to an infinity: canonical, it is a quiet one, whose mark is among the high bits.
     static __device__ __forceinline__ void parts(const float (&v)[8], V (&out)[3]) {
         union { V v8; uint32_t u[4]; } p[3];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            float lo = v[2 * t], hi = v[2 * t + 1];
+            float lo = __builtin_canonicalizef(v[2 * t]), hi = __builtin_canonicalizef(v[2 * t + 1]);
 #pragma unroll
             for (int k = 0; k < 3; ++k) {
                 p[k].u[t] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);

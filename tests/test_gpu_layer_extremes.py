@@ -144,3 +144,37 @@ def test_rates_of_the_lowest_value(lens):
         assert bool(torch.isnan(z[:, 5]).all()) and bool(torch.isnan(held[ran, 5, 3]).all())
         z[:, 5], held[:, 5, 3] = y[:, 5], kept[:, 5, 3]
         assert torch.equal(y, z) and torch.equal(kept, held)
+
+
+# ---- activations of 4-bit products ------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,cin", [(1, 300), (1, 2304), (5, 2304), (20, 300), (300, 300), (1500, 300)])
+def test_every_no_number_stays_one(n, cin):
+    """fp32 no-numbers whose payload lies in their low 16 bits alone, of either sign."""
+    codes = np.random.default_rng(17).integers(1, 8, (300, cin)).astype(np.int8)
+    h = cad.cadnn_q4_pack_codes(codes, np.full((300, -(-cin // 64)), 0.25, np.float32), 64, cad.F32)
+    x = torch.ones(n, cin, device="cuda")
+    clean = cad.cadnn_q4_fc(h, x)
+    for bits in (0x7f800001, 0x7f80ffff, 0x7fc00000, 0xff800001 - 2 ** 32, 0xffffffff - 2 ** 32):
+        x.fill_(1.0)
+        x.view(torch.int32)[n // 2, 5] = bits
+        y = cad.cadnn_q4_fc(h, x)
+        assert bool(torch.isnan(y[n // 2]).all()), hex(bits)
+        y[n // 2] = clean[n // 2]
+        assert torch.equal(y, clean)
+    h.free()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,cin", [(1, 300), (3, 2304), (13, 2304), (20, 300), (300, 304), (300, 301), (1500, 304)])
+def test_fp16_activations_below_the_normal_numbers_count(n, cin):
+    """Products of codes and multiples of 2^-24, whose sums fp32 holds exactly; an fp16 result is rounded to such a multiple once."""
+    g = np.random.default_rng(18)
+    codes = g.integers(-8, 8, (300, cin)).astype(np.int8)
+    h = cad.cadnn_q4_pack_codes(codes, np.full((300, -(-cin // 128)), 0.25, np.float32), 128, cad.F16)
+    x = (g.integers(-1023, 1024, (n, cin)) * 2.0 ** -24).astype(np.float16)
+    y = cad.cadnn_q4_fc(h, dev(x))
+    ref = 0.25 * (x.astype(np.float64) @ codes.astype(np.float64).T)
+    assert (np.abs(y.double().cpu().numpy() - ref) <= half_step(ref, "f16")).all()
+    h.free()
