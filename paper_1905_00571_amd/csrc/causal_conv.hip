@@ -7,6 +7,7 @@
 // 16 bytes of a row (its channels' taps stay in registers) and a run of tokens, over which it slides a window of rows, four
 // rows loaded at a time; K - 1 rows of a run are read twice.  8192 x 4096, K = 4, SiLU: fp16 33 us, 4.1 TB/s, fp32 48 us, 5.6 TB/s
 // (a large copy: 5.5); element by element, where rows are not 16-byte aligned, fp16 37 us.
+#include <algorithm>
 #include <type_traits>
 
 #include "q4.h"
@@ -27,7 +28,7 @@ struct CcArgs {
     int64_t x_stride, y_stride;
     Sequences q;
     int channels, chunk, act, tx_log;
-    int64_t slots;
+    int64_t slots, slot0;
 };
 
 template <typename T, int V, int K>
@@ -35,7 +36,7 @@ __global__ __launch_bounds__(256) void causal_conv_kernel(const CcArgs a) {
     typedef T VT __attribute__((ext_vector_type(V)));
     constexpr int U = 4;
     const int tx = (int)threadIdx.x & ((1 << a.tx_log) - 1);
-    const int64_t slot = (int64_t)blockIdx.x * (256 >> a.tx_log) + ((int)threadIdx.x >> a.tx_log);
+    const int64_t slot = a.slot0 + (int64_t)blockIdx.x * (256 >> a.tx_log) + ((int)threadIdx.x >> a.tx_log);
     const int c = ((int)blockIdx.y * (1 << a.tx_log) + tx) * V;
     if (slot >= a.slots || c >= a.channels) return;
     int piece, lo, hi;
@@ -119,11 +120,17 @@ __global__ __launch_bounds__(256) void causal_conv_kernel(const CcArgs a) {
 }
 
 template <typename T, int V, int K>
-hipError_t launch_cc(const CcArgs& a, hipStream_t s) {
+hipError_t launch_cc(CcArgs a, hipStream_t s) {
     const int vectors = (a.channels + V - 1) / V, tx = 1 << a.tx_log, per = 256 / tx;
-    const dim3 grid((unsigned)((a.slots + per - 1) / per), (unsigned)((vectors + tx - 1) / tx));
-    CADNN_LAUNCH((causal_conv_kernel<T, V, K>), grid, dim3(256), 0, s, a);
-    return hipGetLastError();
+    const int64_t blocks = (a.slots + per - 1) / per, step = 1 << 23;      // (a launch has fewer than 2^32 threads to a row of workgroups)
+    for (int64_t b = 0; b < blocks; b += step) {
+        a.slot0 = b * per;
+        const dim3 grid((unsigned)std::min(step, blocks - b), (unsigned)((vectors + tx - 1) / tx));
+        CADNN_LAUNCH((causal_conv_kernel<T, V, K>), grid, dim3(256), 0, s, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <typename T, int V>

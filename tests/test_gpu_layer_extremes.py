@@ -178,3 +178,24 @@ def test_fp16_activations_below_the_normal_numbers_count(n, cin):
     ref = 0.25 * (x.astype(np.float64) @ codes.astype(np.float64).T)
     assert (np.abs(y.double().cpu().numpy() - ref) <= half_step(ref, "f16")).all()
     h.free()
+
+
+# ---- more work than one launch takes ------------------------------------------------------------------------
+
+@pytest.mark.gpu
+def test_causal_conv1d_of_more_sequences_than_one_launch_has_workgroups_for():
+    """2^24 sequences, all but a few of them empty: 2^24 workgroups of 256 threads are one launch's limit."""
+    seqs, tokens, channels = 1 << 24, 40, 2048
+    g = np.random.default_rng(19)
+    first, middle, end = 7, 9, 24                  # rows of the first sequence, of one in the middle, of the last
+    starts = torch.full((seqs + 1,), first, dtype=torch.int32, device="cuda")
+    starts[0] = 0
+    starts[9_000_001:] = first + middle
+    starts[seqs] = tokens
+    x = g.standard_normal((tokens, channels)).astype(np.float16)
+    w = g.uniform(-1, 1, (channels, 4)).astype(np.float16).astype(np.float32)
+    h = cad.cadnn_pack_weights(w.reshape(channels, 1, 1, 4), cad.F16)
+    want = cad.cadnn_causal_conv1d(h, dev(x), None, dev(np.array([0, first, first + middle, tokens], np.int32)), 3)
+    y = cad.cadnn_causal_conv1d(h, dev(x), None, starts, seqs)
+    assert torch.equal(y, want)
+    h.free()
