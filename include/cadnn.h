@@ -200,6 +200,10 @@ cadnn_status cadnn_q4_prepare(const cadnn_q4_weights* w);
  * another device than the current one); EUNSUPPORTED (n above 2^24); EHIP. */
 cadnn_status cadnn_q4_fc(const cadnn_q4_weights* w, const void* x, int64_t x_stride, void* y, int64_t y_stride, int n,
                          const void* bias, int act, void* stream);
+/* Name of the kernel that serves n rows at x (of which the address alone is looked at), NUL-terminated into buf: "columns_<tokens>",
+ * "few_<filters>x<tokens>" or "tile_<filters>x<tokens>", with a suffix where two kernels have that size.  Host only.
+ * Errors: EINVAL (NULL handle or buffer, n <= 0, x_stride below cin). */
+cadnn_status cadnn_q4_fc_variant_name(const cadnn_q4_weights* w, const void* x, int64_t x_stride, int n, char* buf, size_t len);
 
 /* ------------------------------------------------------------------------- *
  * Layers on packed sequences (no passage of the paper to cite: its models are image networks; these

@@ -103,6 +103,7 @@ def lib() -> ctypes.CDLL:
         "cadnn_q4_unpack": (_i, [_vp, _f32p]),
         "cadnn_q4_prepare": (_i, [_vp]),
         "cadnn_q4_fc": (_i, [_vp, _vp, _i64, _vp, _i64, _i, _vp, _i, _vp]),
+        "cadnn_q4_fc_variant_name": (_i, [_vp, _vp, _i64, _i, ctypes.c_char_p, ctypes.c_size_t]),
         "cadnn_causal_conv1d": (_i, [_vp, _vp, _i64, _vp, _i64, _i, _i, _vp, _vp, _vp, _i, _vp]),
         "cadnn_selective_scan_workspace_bytes": (_i, [ctypes.POINTER(ScanArgs), ctypes.POINTER(ctypes.c_size_t)]),
         "cadnn_selective_scan": (_i, [ctypes.POINTER(ScanArgs), _vp, ctypes.c_size_t, _vp]),
@@ -503,6 +504,13 @@ def cadnn_q4_fc(w: Q4Weights, x, bias=None, act: int = ACT_NONE, out=None, strea
     _check(lib().cadnn_q4_fc(w.handle, x.data_ptr(), x_stride, out.data_ptr(), y_stride, n,
                              None if bias is None else _whole(bias, "bias", _f32(), dev, (cout,)), act, _stream_of(dev)))
     return out
+
+
+def cadnn_q4_fc_variant_name(w: Q4Weights, n: int, x_stride: Optional[int] = None, address: int = 0) -> str:
+    """The kernel that serves n rows, x_stride elements apart (None: cin) from `address` on (of which the alignment counts)."""
+    buf = ctypes.create_string_buffer(64)
+    _check(lib().cadnn_q4_fc_variant_name(w.handle, address, w.cin if x_stride is None else x_stride, n, buf, 64))
+    return buf.value.decode()
 
 
 def cadnn_causal_conv1d(w: Weights, x, state=None, seq_start=None, seqs: int = 1, bias=None, act: int = ACT_NONE,

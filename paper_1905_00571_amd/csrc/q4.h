@@ -25,6 +25,8 @@ constexpr int kQ4Block = 128;     // inputs of a tile; a group (32, 64 or 128) n
 // y = act(x w^T + bias) on rows `x_stride` / `y_stride` elements apart; arguments are checked by the caller.
 cadnn_status launch_q4_fc(const cadnn_q4_weights* w, const void* x, int64_t x_stride, void* y, int64_t y_stride, int n,
                           const float* bias, int act, hipStream_t s);
+// Name of the kernel that serves the rows (the first 2^20 of them).
+const char* q4_fc_variant(const cadnn_q4_weights* w, const void* x, int64_t x_stride, int n);
 // Uploads the device layout, or checks that it is on the current device.  `capturing`: the call's stream, which must
 // not be captured while memory is still to be allocated (NULL: none).
 cadnn_status ensure_q4_device(const cadnn_q4_weights* w, const char* who, hipStream_t capturing, bool has_stream);

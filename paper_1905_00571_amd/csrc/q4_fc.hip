@@ -334,13 +334,12 @@ __global__ __launch_bounds__(512, 4) void q4_columns_kernel(const Q4Args a) {
     }
 }
 
-template <typename T, int GP>
+template <typename T, int GP, int HELD>
 hipError_t launch_columns(const Q4Args& a, hipStream_t s) {
     const int waves = a.blocks >= 8 ? 8 : a.blocks;
     const size_t lds = (size_t)waves * 8192;
     const dim3 grid((unsigned)((a.cout + 15) / 16));
-    if (a.n <= 4) CADNN_LAUNCH((q4_columns_kernel<T, GP, 1>), grid, dim3(64u * waves), lds, s, a);
-    else CADNN_LAUNCH((q4_columns_kernel<T, GP, Q4Frag<T>::kParts == 3 ? 2 : 4>), grid, dim3(64u * waves), lds, s, a);
+    CADNN_LAUNCH((q4_columns_kernel<T, GP, HELD>), grid, dim3(64u * waves), lds, s, a);
     return hipGetLastError();
 }
 
@@ -582,49 +581,99 @@ struct Q4Cost {
     }
 };
 
+// The kernels, as (filters) x (tokens) of a workgroup; tiles with the activations straight to LDS where the call allows it, else through registers.
+enum Q4Kernel {
+    Q4_COLUMNS_FEW,         // 16 filters, 4 tokens
+    Q4_COLUMNS,             // 16 filters, all that one matrix instruction holds: 16 tokens, in fp32 5
+    Q4_FEW_16x16, Q4_FEW_32x16, Q4_FEW_64x16, Q4_FEW_64x32,
+    Q4_TILE_SMALL,          // fp16 64 x 32, fp32 128 x 32
+    Q4_TILE_MIDDLE,         // fp16 128 x 64, fp32 256 x 32
+    Q4_TILE_LARGE,          // fp16 128 x 128 (through registers 128 x 64, one block at a time), fp32 256 x 64
+    Q4_TILE_SMALL_REGISTERS, Q4_TILE_MIDDLE_REGISTERS, Q4_TILE_LARGE_REGISTERS
+};
+
 // Which kernel.  Large tiles read and expand less, but a workgroup alone on its compute unit waits out every latency, and one
 // more than fit costs a round; so the kernels are compared by what they were measured to take (random data, 4096 -> 4096, 33 to 2048
 // tokens; groups of 128, 64, 32).  fp16, 128 x 128 / 128 x 64 / 64 x 32 tiles / few tokens: 128 tokens 50, 22, 13.7, 15; 512 tokens 51,
-// 25, 29, 52; 2048 tokens 76, 85, 115, more.  fp32, 256 x 64 / 256 x 32 / 128 x 32 / few tokens: 128 tokens 90, 51, 34, 22; 512 tokens 91, 54, 57, 81;
+// 25, 29, 52; 2048 tokens 76, 85, 115, more.  fp16 through registers, rows of 4095 inputs, groups of 128 and 32, 128 x 64 one block at a time / 128 x 64 / 64 x 32 /
+// few tokens: 64 tokens 35, 31, 15.6, 18.2 and 46, 37, 17.6, 19.1; 300 tokens 38, 34, 39, 75 and 49, 40, 43, 79; 515 tokens 50, 61, 58, 122 and 62, 77, 63, 133;
+// 2047 tokens of 8190 filters 190, 255, 330, 894 and 264, 311, 365, 954.  (Few tokens where every compute unit has at most one workgroup: with rows of 1001 inputs,
+// 50 tokens of 1000 filters, 5.7 against the small tile's 6.0 and 6.4.)
+// fp32, 256 x 64 / 256 x 32 / 128 x 32 / few tokens: 128 tokens 90, 51, 34, 22; 512 tokens 91, 54, 57, 81;
 // 2048 tokens 198, 216, 218, more.
 template <typename T, int GP>
-hipError_t launch_q4(const Q4Args& a, hipStream_t s) {
+Q4Kernel choose_q4(const Q4Args& a) {
     auto workgroups = [&](int filters, int tokens) { return (int64_t)((a.cout + filters - 1) / filters) * ((a.n + tokens - 1) / tokens); };
     if (a.n > 32) {
         constexpr int G = GP == 1 ? 0 : GP == 2 ? 1 : 2;
         if constexpr (sizeof(T) == 2) {
             // straight to LDS: whole pieces of eight, and 32-bit offsets from the first token of a tile on
             const bool direct = (uintptr_t)a.x % 16 == 0 && a.x_stride % 8 == 0 && a.cin % 8 == 0 && a.x_stride < (1 << 22);
-            constexpr Q4Cost large[3] = {{52, 75, 512}, {52, 83, 512}, {70, 97, 512}}, middle[3] = {{24, 38, 512}, {25, 52, 512}, {36, 65, 512}};
-            constexpr Q4Cost small[3] = {{14, 28, 1024}, {15, 30, 1024}, {18, 37, 1024}}, few[3] = {{11.5, 17, 512}, {12.5, 18.5, 512}, {14, 21, 512}};
-            constexpr Q4Cost large_in_registers[3] = {{38, 45, 512}, {40, 55, 512}, {54, 75, 512}};
-            const double l = direct ? large[G].of(workgroups(128, 128)) : large_in_registers[G].of(workgroups(128, 64));
-            const double m = (direct ? 1.0 : 1.15) * middle[G].of(workgroups(128, 64)), sm = (direct ? 1.0 : 1.15) * small[G].of(workgroups(64, 32));
-            const double f = few[G].of(workgroups(64, 16));
-            if (l <= m && l <= sm && l <= f)
-                return direct ? launch_tile<T, GP, 2, 128, GP == 1 ? 4 : 2, 1, true>(a, s) : launch_tile<T, GP, 2, 64, 4, 1, false>(a, s);
-            if (m <= sm && m <= f) return direct ? launch_tile<T, GP, 2, 64, 4, 2, true>(a, s) : launch_tile<T, GP, 2, 64, 4, 2, false>(a, s);
-            if (sm <= f) return direct ? launch_tile<T, GP, 1, 32, 4, 2, true>(a, s) : launch_tile<T, GP, 1, 32, 4, 2, false>(a, s);
+            if (direct) {
+                constexpr Q4Cost large[3] = {{52, 75, 512}, {52, 83, 512}, {70, 97, 512}}, middle[3] = {{24, 38, 512}, {25, 52, 512}, {36, 65, 512}};
+                constexpr Q4Cost small[3] = {{14, 28, 1024}, {15, 30, 1024}, {18, 37, 1024}}, few[3] = {{11.5, 17, 512}, {12.5, 18.5, 512}, {14, 21, 512}};
+                const double l = large[G].of(workgroups(128, 128)), m = middle[G].of(workgroups(128, 64)), sm = small[G].of(workgroups(64, 32));
+                const double f = few[G].of(workgroups(64, 16));
+                if (l <= m && l <= sm && l <= f) return Q4_TILE_LARGE;
+                if (m <= sm && m <= f) return Q4_TILE_MIDDLE;
+                if (sm <= f) return Q4_TILE_SMALL;
+            } else if (workgroups(64, 16) > 256) {
+                constexpr Q4Cost large[3] = {{38, 56, 512}, {40, 58, 512}, {50, 72, 512}}, middle[3] = {{33.5, 67, 512}, {35, 71, 512}, {41, 82, 512}};
+                constexpr Q4Cost small[3] = {{16.5, 54, 1024}, {17, 55, 1024}, {18.5, 59, 1024}};
+                const double l = large[G].of(workgroups(128, 64)), m = middle[G].of(workgroups(128, 64)), sm = small[G].of(workgroups(64, 32));
+                return l <= m && l <= sm ? Q4_TILE_LARGE_REGISTERS : m <= sm ? Q4_TILE_MIDDLE_REGISTERS : Q4_TILE_SMALL_REGISTERS;
+            }
         } else {
             constexpr Q4Cost large[3] = {{93, 98, 256}, {96, 105, 256}, {106, 115, 256}}, middle[3] = {{52, 54, 256}, {54, 57, 256}, {59, 60, 256}};
             constexpr Q4Cost small[3] = {{38, 29, 256}, {39, 31, 256}, {41, 38, 256}}, few[3] = {{22.5, 20.5, 256}, {22.5, 20.5, 256}, {23, 21, 256}};
             constexpr Q4Cost fewer[3] = {{16.5, 25, 512}, {16.5, 29.5, 512}, {17, 29.5, 512}};
             const double l = large[G].of(workgroups(256, 64)), m = middle[G].of(workgroups(256, 32)), sm = small[G].of(workgroups(128, 32));
             const double f2 = few[G].of(workgroups(64, 32)), f1 = fewer[G].of(workgroups(64, 16)), f = std::min(f1, f2);
-            if (l <= m && l <= sm && l <= f) return launch_tile<T, GP, 4, 64, 2, 2, false>(a, s);
-            if (m <= sm && m <= f) return launch_tile<T, GP, 4, 32, 4, 2, false>(a, s);
-            if (sm <= f) return launch_tile<T, GP, 2, 32, 4, 2, false>(a, s);
-            if (f2 <= f1 && workgroups(64, 32) >= 256) return launch_few<T, GP, 4, 2>(a, s);
+            if (l <= m && l <= sm && l <= f) return Q4_TILE_LARGE;
+            if (m <= sm && m <= f) return Q4_TILE_MIDDLE;
+            if (sm <= f) return Q4_TILE_SMALL;
+            if (f2 <= f1 && workgroups(64, 32) >= 256) return Q4_FEW_64x32;
         }
     }
     // Staged activations pay from rows of some length on (one token, 512 -> 512: fp16 3.5 staged, 2.9 not; 4096 -> 4096: 4.3, 5.7).
-    if (a.n <= 16 / Q4Frag<T>::kParts && a.blocks > (sizeof(T) == 2 ? 16 : 8)) return launch_columns<T, GP>(a, s);
+    if (a.n <= 16 / Q4Frag<T>::kParts && a.blocks > (sizeof(T) == 2 ? 16 : 8)) return a.n <= 4 ? Q4_COLUMNS_FEW : Q4_COLUMNS;
     // (13 tokens, 5003 -> 4099, groups of 32, fp16: one tile of filters a wave 22.5, two 14.5; 4096 filters, one 13.5, two 14.5)
-    if (a.n <= 16) return a.cout > 16 * 256 && a.blocks > 8 ? launch_few<T, GP, 2, 1>(a, s) : launch_few<T, GP, 1, 1>(a, s);
+    if (a.n <= 16) return a.cout > 16 * 256 && a.blocks > 8 ? Q4_FEW_32x16 : Q4_FEW_16x16;
     constexpr bool h = sizeof(T) == 2;
     constexpr Q4Cost few1 = {h ? 7.3 : 11.3, h ? 12.5 : 20, 512}, few2 = {h ? 9.3 : 11.8, h ? 13 : 21.5, 512}, few4 = {h ? 11.5 : 16.5, h ? 16.5 : 27, 512};
     const double f1 = few1.of(workgroups(16, 16)), f2 = few2.of(workgroups(32, 16)), f4 = few4.of(workgroups(64, 16));
-    return f4 <= f2 && f4 <= f1 ? launch_few<T, GP, 4, 1>(a, s) : f2 <= f1 ? launch_few<T, GP, 2, 1>(a, s) : launch_few<T, GP, 1, 1>(a, s);
+    return f4 <= f2 && f4 <= f1 ? Q4_FEW_64x16 : f2 <= f1 ? Q4_FEW_32x16 : Q4_FEW_16x16;
+}
+
+template <typename T, int GP>
+hipError_t launch_q4(const Q4Args& a, hipStream_t s) {
+    constexpr bool h = sizeof(T) == 2;
+    const Q4Kernel kernel = choose_q4<T, GP>(a);
+    switch (kernel) {
+        case Q4_COLUMNS_FEW: return launch_columns<T, GP, 1>(a, s);
+        case Q4_COLUMNS: return launch_columns<T, GP, h ? 4 : 2>(a, s);
+        case Q4_FEW_16x16: return launch_few<T, GP, 1, 1>(a, s);
+        case Q4_FEW_32x16: return launch_few<T, GP, 2, 1>(a, s);
+        case Q4_FEW_64x16: return launch_few<T, GP, 4, 1>(a, s);
+        default: break;
+    }
+    if constexpr (h) {
+        switch (kernel) {
+            case Q4_TILE_SMALL: return launch_tile<T, GP, 1, 32, 4, 2, true>(a, s);
+            case Q4_TILE_MIDDLE: return launch_tile<T, GP, 2, 64, 4, 2, true>(a, s);
+            case Q4_TILE_LARGE: return launch_tile<T, GP, 2, 128, GP == 1 ? 4 : 2, 1, true>(a, s);
+            case Q4_TILE_SMALL_REGISTERS: return launch_tile<T, GP, 1, 32, 4, 2, false>(a, s);
+            case Q4_TILE_MIDDLE_REGISTERS: return launch_tile<T, GP, 2, 64, 4, 2, false>(a, s);
+            default: return launch_tile<T, GP, 2, 64, 4, 1, false>(a, s);
+        }
+    } else {
+        switch (kernel) {
+            case Q4_FEW_64x32: return launch_few<T, GP, 4, 2>(a, s);
+            case Q4_TILE_SMALL: return launch_tile<T, GP, 2, 32, 4, 2, false>(a, s);
+            case Q4_TILE_MIDDLE: return launch_tile<T, GP, 4, 32, 4, 2, false>(a, s);
+            default: return launch_tile<T, GP, 4, 64, 2, 2, false>(a, s);
+        }
+    }
 }
 
 template <typename T>
@@ -632,19 +681,51 @@ hipError_t launch_q4_group(const Q4Args& a, int group, hipStream_t s) {
     return group == 128 ? launch_q4<T, 1>(a, s) : group == 64 ? launch_q4<T, 2>(a, s) : launch_q4<T, 4>(a, s);
 }
 
+template <typename T>
+Q4Kernel choose_q4_group(const Q4Args& a, int group) {
+    return group == 128 ? choose_q4<T, 1>(a) : group == 64 ? choose_q4<T, 2>(a) : choose_q4<T, 4>(a);
+}
+
+// A launch has at most 65535 rows of workgroups.
+constexpr int kQ4LaunchRows = 16 * 65535;
+
+// What choice and launch need of a call's first rows.
+Q4Args q4_args(const cadnn_q4_weights* w, const void* x, int64_t x_stride, int n) {
+    Q4Args a{};
+    a.codes = (const uint32_t*)w->d_codes.p; a.scales = w->d_scales.p;
+    a.x = x; a.x_stride = x_stride;
+    a.n = std::min(kQ4LaunchRows, n); a.cin = w->cin; a.cout = w->cout; a.blocks = (w->cin + kQ4Block - 1) / kQ4Block;
+    return a;
+}
+
 }  // namespace
+
+const char* q4_fc_variant(const cadnn_q4_weights* w, const void* x, int64_t x_stride, int n) {
+    const Q4Args a = q4_args(w, x, x_stride, n);
+    const bool h = w->dtype == CADNN_F16;
+    switch (h ? choose_q4_group<_Float16>(a, w->group) : choose_q4_group<float>(a, w->group)) {
+        case Q4_COLUMNS_FEW: return "columns_4";
+        case Q4_COLUMNS: return h ? "columns_16" : "columns_5";
+        case Q4_FEW_16x16: return "few_16x16";
+        case Q4_FEW_32x16: return "few_32x16";
+        case Q4_FEW_64x16: return "few_64x16";
+        case Q4_FEW_64x32: return "few_64x32";
+        case Q4_TILE_SMALL: return h ? "tile_64x32_lds" : "tile_128x32";
+        case Q4_TILE_MIDDLE: return h ? "tile_128x64_lds" : "tile_256x32";
+        case Q4_TILE_LARGE: return h ? "tile_128x128_lds" : "tile_256x64";
+        case Q4_TILE_SMALL_REGISTERS: return "tile_64x32";
+        case Q4_TILE_MIDDLE_REGISTERS: return "tile_128x64";
+        default: return "tile_128x64_whole";
+    }
+}
 
 cadnn_status launch_q4_fc(const cadnn_q4_weights* w, const void* x, int64_t x_stride, void* y, int64_t y_stride, int n,
                           const float* bias, int act, hipStream_t s) {
     const size_t e = w->elem();
-    // a launch has at most 65535 rows of workgroups
-    const int step = 16 * 65535;
-    for (int n0 = 0; n0 < n; n0 += step) {
-        Q4Args a{};
-        a.codes = (const uint32_t*)w->d_codes.p; a.scales = w->d_scales.p; a.bias = bias;
-        a.x = (const char*)x + (size_t)n0 * x_stride * e; a.y = (char*)y + (size_t)n0 * y_stride * e;
-        a.x_stride = x_stride; a.y_stride = y_stride;
-        a.n = std::min(step, n - n0); a.cin = w->cin; a.cout = w->cout; a.blocks = (w->cin + kQ4Block - 1) / kQ4Block; a.act = act;
+    for (int n0 = 0; n0 < n; n0 += kQ4LaunchRows) {
+        Q4Args a = q4_args(w, (const char*)x + (size_t)n0 * x_stride * e, x_stride, n - n0);
+        a.y = (char*)y + (size_t)n0 * y_stride * e; a.y_stride = y_stride;
+        a.bias = bias; a.act = act;
         CADNN_HIP(w->dtype == CADNN_F16 ? launch_q4_group<_Float16>(a, w->group, s) : launch_q4_group<float>(a, w->group, s));
     }
     return CADNN_OK;

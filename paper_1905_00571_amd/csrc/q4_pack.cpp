@@ -238,3 +238,11 @@ extern "C" cadnn_status cadnn_q4_fc(const cadnn_q4_weights* w, const void* x, in
     if (st != CADNN_OK) return st;
     return launch_q4_fc(w, x, x_stride, y, y_stride, n, (const float*)bias, act, (hipStream_t)stream);
 }
+
+extern "C" cadnn_status cadnn_q4_fc_variant_name(const cadnn_q4_weights* w, const void* x, int64_t x_stride, int n, char* buf, size_t len) {
+    if (!w || !buf || len == 0) return fail(CADNN_EINVAL, "cadnn_q4_fc_variant_name: NULL pointer");
+    if (n <= 0 || x_stride < w->cin) return fail(CADNN_EINVAL, "cadnn_q4_fc_variant_name: non-positive number of rows, or rows that overlap");
+    std::strncpy(buf, q4_fc_variant(w, x, x_stride, n), len - 1);
+    buf[len - 1] = '\0';
+    return CADNN_OK;
+}
