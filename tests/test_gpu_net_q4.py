@@ -79,6 +79,33 @@ def test_4bit_classifier_on_channels_last_tensors():
     net.free()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("name,shape", [("small", (1, 16, 14, 14)), ("small", (40, 16, 28, 28)), ("flat", (1, 16, 14, 14)), ("flat", (5, 16, 14, 14))])
+@pytest.mark.parametrize("quant", [("fc1", "fc2"), ("fc2",)])
+def test_4bit_classifier_behind_pinned_channels_last_convolutions(dtype, name, shape, quant):
+    """The pin takes the whole net to channels-last tensors, whichever execution it would have had; 4-bit layers read vectors and flat feature maps there."""
+    flag, tol = (cad.F16, TOL_F16) if dtype == "f16" else (cad.F32, TOL_F32)
+    ops = small_net(0.5) if name == "small" else flat_net()
+    x, ws, bs = wl.net_tensors(ops, "q4net-pin-" + name, shape, input_relu=True)
+    mixed, plain = quantised(ops, ws, quant, 64, flag)
+    ref, _, _ = oracle.run_net(ops, x, plain, bs)
+    xd = torch.from_numpy(x).cuda()
+    xd = xd.half() if flag == cad.F16 else xd
+    for use_graph in (False, True):
+        net = cad.build_net(ops, mixed, bs, shape, flag, use_graph=use_graph)
+        net.set_op_variant(0, "cl_mfma_64x64_s3")
+        names = net.variants()
+        assert all(names[i].startswith("cl_") or names[i] == "fused" for i, op in enumerate(ops) if op.kind == "conv"), names
+        assert [names[i] for i, op in enumerate(ops) if op.kind == "fc"] == ["q4fc" if op.name in quant else "sfc" for op in ops if op.kind == "fc"]
+        for _ in range(3):
+            assert_net_close(net.run(xd).float().cpu().numpy().reshape(ref.shape), ref, tol, str(use_graph))
+        net.free()
+    for w in mixed:
+        if isinstance(w, cad.Q4Weights):
+            w.free()
+
+
 def test_net_with_4bit_layer_is_planned_and_checked_without_a_gpu():
     ops = small_net(0.8)
     shape = (2, 16, 14, 14)
