@@ -199,3 +199,29 @@ def test_causal_conv1d_of_more_sequences_than_one_launch_has_workgroups_for():
     y = cad.cadnn_causal_conv1d(h, dev(x), None, starts, seqs)
     assert torch.equal(y, want)
     h.free()
+
+
+# ---- gates of a scan -------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("tokens", [1, 3, 20, 400])
+@pytest.mark.parametrize("dstate", [4, 40])
+def test_gate_of_a_scan_at_the_ends_of_its_range(dtype, tokens, dstate):
+    """Outputs that are the gate alone (d x = 1, c = 0): in fp32 as exact as the other layers' SiLU, in fp16 to a half step and 3 |z| half steps of fp32."""
+    tt, flag, npt = TYPES[dtype]
+    with np.errstate(over="ignore"):
+        z = np.concatenate([ENDS, np.linspace(-87, 87, 229)]).astype(npt)
+    v = scan_inputs([tokens], len(z), dstate, 1, npt, 20)
+    v["x"][:], v["c"][:], v["z"][:], v["d"][:] = 1.0, 0.0, z, 1.0
+    for how in ({}, {"workspace": torch.empty(0, dtype=torch.uint8, device="cuda")}):
+        y, _ = run_scan(v, None, 1, **how)
+        for row in {0, tokens // 2, tokens - 1}:
+            if dtype == "f32":
+                check_silu(y[row], z, dtype)
+            else:
+                f = np.isfinite(z) & (np.abs(z) < 65504)
+                ref = z[f].astype(np.float64) / (1 + np.exp(-np.clip(z[f].astype(np.float64), -700, None)))
+                got = y[row].double().cpu().numpy()
+                assert (np.abs(got[f] - ref) <= (8 + 3 * np.abs(z[f])) * U * np.abs(ref) + half_step(ref, dtype)).all()
+                assert np.array_equal(np.isnan(got), np.isnan(z) | (z == -np.inf)) and (got[z == np.inf] == np.inf).all()
