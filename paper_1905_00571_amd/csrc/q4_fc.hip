@@ -570,8 +570,8 @@ hipError_t launch_tile(const Q4Args& a, hipStream_t s) {
 }
 
 // What a kernel takes, in us for rows of 4096 inputs, from the number of its workgroups: `one` while every compute unit has at
-// most one, then `full` for every `fit` of them, the last ones included, which run `fit` at a time -- or, small as they are
-// (1024 to a round), for as many as there are.
+// most one, then `full` for every `fit` of them, the last ones included, which run `fit` at a time -- or, where their times were in
+// proportion to their number (1024 to `full`), for as many as there are.
 struct Q4Cost {
     double one, full;
     int fit;
@@ -618,7 +618,7 @@ Q4Kernel choose_q4(const Q4Args& a) {
                 if (m <= sm && m <= f) return Q4_TILE_MIDDLE;
                 if (sm <= f) return Q4_TILE_SMALL;
             } else if (workgroups(64, 16) > 256) {
-                constexpr Q4Cost large[3] = {{38, 56, 512}, {40, 58, 512}, {50, 72, 512}}, middle[3] = {{33.5, 67, 512}, {35, 71, 512}, {41, 82, 512}};
+                constexpr Q4Cost large[3] = {{38, 110, 1024}, {40, 113, 1024}, {50, 142, 1024}}, middle[3] = {{33.5, 67, 512}, {35, 71, 512}, {41, 82, 512}};
                 constexpr Q4Cost small[3] = {{16.5, 54, 1024}, {17, 55, 1024}, {18.5, 59, 1024}};
                 const double l = large[G].of(workgroups(128, 64)), m = middle[G].of(workgroups(128, 64)), sm = small[G].of(workgroups(64, 32));
                 return l <= m && l <= sm ? Q4_TILE_LARGE_REGISTERS : m <= sm ? Q4_TILE_MIDDLE_REGISTERS : Q4_TILE_SMALL_REGISTERS;
