@@ -5,8 +5,8 @@
 // where x~ before a sequence's first token is its tail, the last K - 1 rows that earlier calls saw.  The layer moves every
 // element once and does K multiply-adds with it: memory bounds it, and the launch itself for single tokens.  A thread owns
 // 16 bytes of a row (its channels' taps stay in registers) and a run of tokens, over which it slides a window of rows, four
-// rows loaded at a time; K - 1 rows of a run are read twice.  8192 x 4096, K = 4, SiLU: fp16 33 us, 4.1 TB/s, fp32 48 us, 5.6 TB/s
-// (a large copy: 5.5); element by element, where rows are not 16-byte aligned, fp16 37 us.
+// rows loaded at a time; K - 1 rows of a run are read twice.  8192 x 4096, K = 4, SiLU, three sets of tensors in turn: fp16 33.5 us, 4.0 TB/s, fp32
+// 47 us, 5.7 TB/s (a large copy: 5.1 to 5.5); element by element, where rows are not 16-byte aligned, fp16 36 us.
 #include <algorithm>
 #include <type_traits>
 

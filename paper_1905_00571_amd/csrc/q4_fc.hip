@@ -72,7 +72,8 @@ template <> struct Q4Frag<float> {
     }
     // The parts are cut off, not rounded, so that a large value's first part stays finite; what is left of an infinity
     // (no number) is replaced by a finite value that the infinity swallows.  A no-number that keeps its payload in its low bits, all of them
-    // signalling, would be cut to an infinity: canonical, it is a quiet one, whose mark is among the high bits.
+    // signalling, would be cut to an infinity: canonical, it is a quiet one, whose mark is among the high bits.  (3 tokens 25088 -> 4096, groups of 32,
+    // 25.3 us so, 24.6 without; pairs compared, and made canonical behind a branch, 26.3.)
     static __device__ __forceinline__ void parts(const float (&v)[8], V (&out)[3]) {
         union { V v8; uint32_t u[4]; } p[3];
 #pragma unroll
@@ -232,7 +233,7 @@ __global__ __launch_bounds__(512) void q4_few_kernel(const Q4Args a) {
 // As many tokens as one matrix instruction has columns: 16 in fp16, five in fp32, where the three parts of a token take three
 // columns and one instruction serves all of them.  The workgroup brings the activations of a chunk (one block for every
 // wave) into LDS, each element read, and cut apart, once, while the matrix instructions work on the chunk before, and a wave's
-// codes and scales are fetched D chunks ahead.  us at 8192 -> 8192, groups of 128, one token: fp16 8.9, fp32 11.8, where the kernel above
+// codes and scales are fetched D chunks ahead.  us at 8192 -> 8192, groups of 128, one token: fp16 8.7, fp32 11.7, where the kernel above
 // takes 14.1 and 19.0; the 35 MB are 6.4 us at the rate of a large copy.  (Fetched 3, 4, 8 chunks ahead, which repeats the last block as often behind the
 // end: fp16 9.4, 9.8, 11.7; not fetched there, by a branch: 9.7, as what is waited for is then less well known.)
 // (Two workgroups to a compute unit, which takes 128 registers: with one, the 257 tiles of 4099 filters took twice the time of 256.)
@@ -360,7 +361,7 @@ hipError_t launch_few(const Q4Args& a, hipStream_t s) {
 // tokens meet all banks.  KS steps of 32 inputs are expanded at a time; their sums start from zero in the first matrix
 // instruction and are multiplied by the group's scale into the fp32 accumulators, which for groups of 32 is as much vector
 // work as there is matrix work.  (With the scale multiplied into the codes, rounded to fp16, 2048 tokens through 4096 -> 8192 took 128 us for
-// any group, where this takes 143, 151 and 181 for groups of 128, 64 and 32; the library's fp16 product takes 114.)  WK = 2: two
+// any group, where this takes 137 to 143, 147 to 151 and 168 to 173 for groups of 128, 64 and 32; the library's fp16 product takes 108 to 114.)  WK = 2: two
 // times four waves take the blocks in turn and add up, where there are too few workgroups to wait for each other's loads.
 // DIRECT (fp16): activations go straight to LDS, into the second of two buffers, else through registers.
 template <typename T, int GP, int RW, int BN, int KS, int WK, bool DIRECT>

@@ -8,8 +8,8 @@
 // SIMD per 64 of them, against 4 / N elements of traffic: from N = 16 on the vector units bound a long scan, and the
 // states' traffic a single token.  A long sequence is a chain of tokens that only channels and states run beside, so it is cut into
 // pieces: one pass for what each piece ends with, a join, one for the outputs -- the exponentials are taken twice.  us at 4096
-// tokens x 2048 channels x 16 states, gated, fp16: 33 + 11 + 41 (four waves a SIMD; 20 for the vector work of one pass at its rate, 12 for the
-// traffic); one token of 64 sequences x 4096 x 16: 11.8, 3.1 TB/s.
+// tokens x 2048 channels x 16 states, gated, fp16: 30 + 11 + 38 (four waves a SIMD; 20 for the vector work of one pass at its rate, 12 for the
+// traffic); one token of 64 sequences x 4096 x 16: 10.4, 3.5 TB/s.
 #include <type_traits>
 
 #include "q4.h"
