@@ -237,7 +237,7 @@ cadnn_status cadnn_causal_conv1d(const cadnn_weights* w, const void* x, int64_t 
 
 /* Selective state space scan: for every row t, channel c and state n < dstate
  *
- *   step = dt[t][c] + dt_bias[c], and log(1 + exp(step)) of that if `softplus`
+ *   step = dt[t][c] + dt_bias[c], and log(1 + exp(step)) of that if `softplus`     (below 2^127 in magnitude, over a sequence as well)
  *   h[c][n] = exp(step * a[c][n]) * h[c][n] + step * x[t][c] * b[t][g][n]      g = c / (channels / groups)
  *   y[t][c] = (sum_n c[t][g][n] * h[c][n] + d[c] * x[t][c]) * silu(z[t][c])
  *

@@ -221,7 +221,7 @@ def test_gate_of_a_scan_at_the_ends_of_its_range(dtype, tokens, dstate):
                 check_silu(y[row], z, dtype)
             else:
                 f = np.isfinite(z) & (np.abs(z) < 65504)
-                ref = z[f].astype(np.float64) / (1 + np.exp(-np.clip(z[f].astype(np.float64), -700, None)))
-                got = y[row].double().cpu().numpy()
-                assert (np.abs(got[f] - ref) <= (8 + 3 * np.abs(z[f])) * U * np.abs(ref) + half_step(ref, dtype)).all()
+                zf, got = z[f].astype(np.float64), y[row].double().cpu().numpy()
+                ref = zf / (1 + np.exp(-np.clip(zf, -700, None)))
+                assert (np.abs(got[f] - ref) <= (8 + 3 * np.abs(zf)) * U * np.abs(ref) + half_step(ref, dtype)).all()
                 assert np.array_equal(np.isnan(got), np.isnan(z) | (z == -np.inf)) and (got[z == np.inf] == np.inf).all()
